@@ -1,4 +1,4 @@
-"""ctypes binding of libhetis_attn.so: same names as include/hetis_attn.h and include/hetis_kv.h.
+"""ctypes binding of libhetis_attn.so: same names as the headers in include/.
 
 Argument marshalling only.  Tensors are torch tensors that already live on the
 GPU (PyTorch is used for device memory and streams, nothing else); every
@@ -31,6 +31,7 @@ HETIS_ERR_INFEASIBLE = -9
 HETIS_ERR_DEVICE_WAIT = -10
 HETIS_ATTN_CONTROL_BYTES = 256
 HETIS_ATTN_STATIC_SCRATCH_BYTES = 32 << 20
+HETIS_KV4_GROUP = 32
 
 
 class hetis_attn_shape(C.Structure):
@@ -154,6 +155,32 @@ def load(build_if_missing: bool = False):
     lib.hetis_kv_copy_tiles.argtypes = [pool, vp, vp, pool, vp, vp, vp, vp, i32, vp, vp, i32, vp]
     lib.hetis_kv_profile_events.restype = C.c_int
     lib.hetis_kv_profile_events.argtypes = [vp, vp]
+    lib.hetis_kv4_tile_bytes.restype = C.c_int
+    lib.hetis_kv4_tile_bytes.argtypes = [i32]
+    lib.hetis_kv4_append.restype = C.c_int
+    lib.hetis_kv4_append.argtypes = lib.hetis_kv_append.argtypes
+    lib.hetis_kv4_store.restype = C.c_int
+    lib.hetis_kv4_store.argtypes = lib.hetis_kv_store.argtypes
+    lib.hetis_kv4_fetch.restype = C.c_int
+    lib.hetis_kv4_fetch.argtypes = lib.hetis_kv_fetch.argtypes
+    lib.hetis_attn_decode_kv4.restype = C.c_int
+    lib.hetis_attn_decode_kv4.argtypes = lib.hetis_attn_decode.argtypes
+    lib.hetis_attn_decode_kv4_ws.restype = C.c_int
+    lib.hetis_attn_decode_kv4_ws.argtypes = lib.hetis_attn_decode_ws.argtypes
+    for name in ("hetis_attn_decode_weights", "hetis_attn_decode_kv4_weights"):
+        fn, ws = getattr(lib, name), getattr(lib, name + "_ws")
+        fn.restype = ws.restype = C.c_int
+        fn.argtypes = [shp, vp, vp, vp, vp, vp, vp, i32, f32, f32, vp, vp, vp, vp, vp, vp]
+        ws.argtypes = [shp, vp, vp, vp, vp, vp, vp, i32, f32, f32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.hetis_attn_decode_kv4_workspace_bytes.restype = C.c_int
+    lib.hetis_attn_decode_kv4_workspace_bytes.argtypes = [shp, i32, C.POINTER(C.c_size_t)]
+    lib.hetis_attn_decode_weights_workspace_bytes.restype = C.c_int
+    lib.hetis_attn_decode_weights_workspace_bytes.argtypes = [shp, i32, C.POINTER(C.c_size_t)]
+    lib.hetis_kv_evict.restype = C.c_int
+    lib.hetis_kv_evict.argtypes = [shp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    for name in ("hetis_kv_move", "hetis_kv4_move"):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = [shp, vp, vp, i32, vp, vp, i32, i64, vp, vp, vp]
     lib.call = _Calls(lib)
     _lib = lib
     return lib
@@ -174,7 +201,10 @@ class _Calls:
                      "hetis_attn_decode_pairs_step", "hetis_attn_decode_pairs_step_ws",
                      "hetis_attn_decode_split", "hetis_attn_decode_split_ws", "hetis_attn_merge",
                      "hetis_kv_append", "hetis_kv_append_pairs", "hetis_kv_store", "hetis_kv_fetch",
-                     "hetis_kv_copy_tiles"):
+                     "hetis_kv_copy_tiles", "hetis_attn_decode_kv4", "hetis_attn_decode_kv4_ws",
+                     "hetis_kv4_append", "hetis_kv4_store", "hetis_kv4_fetch", "hetis_attn_decode_weights",
+                     "hetis_attn_decode_weights_ws", "hetis_attn_decode_kv4_weights",
+                     "hetis_attn_decode_kv4_weights_ws", "hetis_kv_evict", "hetis_kv_move", "hetis_kv4_move"):
             fn = getattr(lib, name)
             setattr(self, name, _marshal.bind(name, C.cast(fn, C.c_void_p).value) if native else _by_ctypes(fn))
 
@@ -430,6 +460,106 @@ def hetis_kv_copy_tiles(src_pool, src_k, src_v, dst_pool, dst_k, dst_v, src_bloc
 def hetis_kv_profile_events(begin, end) -> int:
     """begin/end: raw hipEvent_t handles (ints) or None."""
     return load().hetis_kv_profile_events(begin, end)
+
+
+def hetis_kv4_tile_bytes(head_dim: int) -> int:
+    return load().hetis_kv4_tile_bytes(int(head_dim))
+
+
+def hetis_kv4_append(shape, k_new, v_new, block_table, seq_lens, head_ids, n_sel_heads, num_blocks,
+                     k_cache, v_cache, stream=None) -> int:
+    return (_lib or load()).call.hetis_kv4_append(shape, k_new, v_new, block_table, seq_lens,
+        head_ids, n_sel_heads, num_blocks, k_cache, v_cache, _stream(stream))
+
+
+def hetis_kv4_store(shape, k_new, v_new, token_seq, token_pos, n_tokens, block_table, head_ids,
+                    n_sel_heads, num_blocks, k_cache, v_cache, stream=None) -> int:
+    return (_lib or load()).call.hetis_kv4_store(shape, k_new, v_new, token_seq, token_pos, n_tokens,
+        block_table, head_ids, n_sel_heads, num_blocks, k_cache, v_cache, _stream(stream))
+
+
+def hetis_kv4_fetch(shape, k_cache, v_cache, token_seq, token_pos, n_tokens, block_table, head_ids,
+                    n_sel_heads, num_blocks, k_out, v_out, stream=None) -> int:
+    return (_lib or load()).call.hetis_kv4_fetch(shape, k_cache, v_cache, token_seq, token_pos,
+        n_tokens, block_table, head_ids, n_sel_heads, num_blocks, k_out, v_out, _stream(stream))
+
+
+def hetis_attn_decode_kv4(shape, q, k_cache, v_cache, block_table, seq_lens, head_ids, n_sel_heads,
+                          scale, out, stream=None) -> int:
+    return (_lib or load()).call.hetis_attn_decode_kv4(shape, q, k_cache, v_cache, block_table,
+        seq_lens, head_ids, n_sel_heads, scale, out, _stream(stream))
+
+
+def hetis_attn_decode_kv4_ws(shape, q, k_cache, v_cache, block_table, seq_lens, head_ids,
+                             n_sel_heads, scale, out, workspace, workspace_bytes, stream=None) -> int:
+    return (_lib or load()).call.hetis_attn_decode_kv4_ws(shape, q, k_cache, v_cache, block_table,
+        seq_lens, head_ids, n_sel_heads, scale, out, workspace, workspace_bytes, _stream(stream))
+
+
+def hetis_attn_decode_kv4_workspace_bytes(shape, n_sel_heads):
+    """(status, bytes)."""
+    n = C.c_size_t(0)
+    rc = load().hetis_attn_decode_kv4_workspace_bytes(C.byref(shape), int(n_sel_heads), C.byref(n))
+    return rc, n.value
+
+
+def hetis_attn_decode_weights(shape, q, k_cache, v_cache, block_table, seq_lens, head_ids,
+                              n_sel_heads, scale, decay, weights_in, n_seen, out, weights_out,
+                              positions, stream=None) -> int:
+    return (_lib or load()).call.hetis_attn_decode_weights(shape, q, k_cache, v_cache, block_table,
+        seq_lens, head_ids, n_sel_heads, scale, decay, weights_in, n_seen, out, weights_out,
+        positions, _stream(stream))
+
+
+def hetis_attn_decode_weights_ws(shape, q, k_cache, v_cache, block_table, seq_lens, head_ids,
+                                 n_sel_heads, scale, decay, weights_in, n_seen, out, weights_out,
+                                 positions, workspace, workspace_bytes, stream=None) -> int:
+    return (_lib or load()).call.hetis_attn_decode_weights_ws(shape, q, k_cache, v_cache, block_table,
+        seq_lens, head_ids, n_sel_heads, scale, decay, weights_in, n_seen, out, weights_out,
+        positions, workspace, workspace_bytes, _stream(stream))
+
+
+def hetis_attn_decode_kv4_weights(shape, q, k_cache, v_cache, block_table, seq_lens, head_ids,
+                                  n_sel_heads, scale, decay, weights_in, n_seen, out, weights_out,
+                                  positions, stream=None) -> int:
+    return (_lib or load()).call.hetis_attn_decode_kv4_weights(shape, q, k_cache, v_cache, block_table,
+        seq_lens, head_ids, n_sel_heads, scale, decay, weights_in, n_seen, out, weights_out,
+        positions, _stream(stream))
+
+
+def hetis_attn_decode_kv4_weights_ws(shape, q, k_cache, v_cache, block_table, seq_lens, head_ids,
+                                     n_sel_heads, scale, decay, weights_in, n_seen, out, weights_out,
+                                     positions, workspace, workspace_bytes, stream=None) -> int:
+    return (_lib or load()).call.hetis_attn_decode_kv4_weights_ws(shape, q, k_cache, v_cache,
+        block_table, seq_lens, head_ids, n_sel_heads, scale, decay, weights_in, n_seen, out,
+        weights_out, positions, workspace, workspace_bytes, _stream(stream))
+
+
+def hetis_attn_decode_weights_workspace_bytes(shape, n_sel_heads):
+    """(status, bytes)."""
+    n = C.c_size_t(0)
+    rc = load().hetis_attn_decode_weights_workspace_bytes(C.byref(shape), int(n_sel_heads), C.byref(n))
+    return rc, n.value
+
+
+def hetis_kv_evict(shape, weights_in, positions_in, seq_lens, n_seen, budgets, head_ids, n_sel_heads,
+                   n_sink, n_recent, max_moves, weights_out, positions_out, new_lens, move_src,
+                   move_dst, stream=None) -> int:
+    return (_lib or load()).call.hetis_kv_evict(shape, weights_in, positions_in, seq_lens, n_seen,
+        budgets, head_ids, n_sel_heads, n_sink, n_recent, max_moves, weights_out, positions_out,
+        new_lens, move_src, move_dst, _stream(stream))
+
+
+def hetis_kv_move(shape, move_src, move_dst, max_moves, block_table, head_ids, n_sel_heads,
+                  num_blocks, k_cache, v_cache, stream=None) -> int:
+    return (_lib or load()).call.hetis_kv_move(shape, move_src, move_dst, max_moves, block_table,
+        head_ids, n_sel_heads, num_blocks, k_cache, v_cache, _stream(stream))
+
+
+def hetis_kv4_move(shape, move_src, move_dst, max_moves, block_table, head_ids, n_sel_heads,
+                   num_blocks, k_cache, v_cache, stream=None) -> int:
+    return (_lib or load()).call.hetis_kv4_move(shape, move_src, move_dst, max_moves, block_table,
+        head_ids, n_sel_heads, num_blocks, k_cache, v_cache, _stream(stream))
 
 
 def hetis_profiler_fit(h, g, tau, n, abc, accuracy=None) -> int:

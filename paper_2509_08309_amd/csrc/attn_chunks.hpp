@@ -1,0 +1,434 @@
+// Decode Attention over the 4-bit cache, and decode Attention that also accumulates attention weight
+// (either cache).  All of it goes to the matrix cores, r = 1 included: the vector units are busy turning
+// codes into fp16 values, and the padded columns of a 16-column product cost the matrix cores nothing that
+// anything else waits for.
+//
+//   S^T = K . Q^T      v_mfma_f32_16x16x32_f16.  Lane l = 16 q + n holds dims q D/4 .. of token n (A) and of
+//                      query head n (B): one run of a K row, which lies in one group of 32 values.
+//   O^T += V^T . P     v_mfma_f32_16x16x32_f16 over 32 tokens: lane l holds, of tokens 4 q .. 4 q + 3 of both
+//                      tiles, dim n D/16 + j (A, row block j) and the probabilities of head n (B), which are
+//                      what the first product and exp2 leave in its registers.
+//
+// A row (sequence, head) is cut into chunks of kCkTokens tokens, always at the same places; the four waves
+// of a workgroup take a quarter of a chunk's tile pairs each and fold their sums through LDS.  Rows of more
+// than one chunk leave fp32 partial results that a second kernel combines.
+#pragma once
+#include "attn_common.hpp"
+#include "kv4_cache.hpp"
+
+namespace hetis {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kCkTokens = 512;
+constexpr int kCkWaves = 4;
+constexpr int kCkThreads = 64 * kCkWaves;
+constexpr int kCkMaxGroup = 8;              // query heads of a KV head
+constexpr int kCkTiles = kCkTokens / kBlockTokens;
+
+struct ChunkParams {
+    const __half *q;                        // [B, Hq, D]
+    const unsigned char *k, *v;
+    const int32_t *block_table, *seq_lens, *head_ids;
+    __half *out;                            // [B, Hq, D]
+    float *o_partial;                       // [B, n_sel, max_chunks, r, D], normalised
+    float *lse_partial;                     // [B, n_sel, max_chunks, r], base 2
+    float *scores;                          // [B, n_sel, r, slots], base 2 (weights only)
+    // weights only
+    const float *w_in;                      // or nullptr
+    const int32_t *n_seen;                  // or nullptr
+    float *w_out;
+    int32_t *positions;
+    int64_t stride_block, stride_head;      // bytes
+    int32_t batch, n_sel, n_q_heads, n_kv_heads, group, max_blocks_per_seq, max_chunks, slots;
+    float scale_log2, decay;
+};
+
+__device__ __forceinline__ int chunks_of(int L) { return max((L + kCkTokens - 1) / kCkTokens, 1); }
+
+// ---- what a lane loads of two neighbouring tiles, and the operands it makes of it
+
+template <int D>
+struct Kv4Pair {
+    static constexpr int KW = D / 32;                          // words of K codes: a quarter of a row
+    typedef unsigned int Words __attribute__((ext_vector_type(KW)));
+    Words kc[2], vc[2];
+    unsigned kp[2];                                            // (s, b) of the group
+    u32x4 vp[2];                                               // scales of the four tokens, biases
+
+    static constexpr int kTileBytes = kv4_tile_bytes(D);
+    __device__ __forceinline__ void issue(int t, __amdgpu_buffer_rsrc_t rk, __amdgpu_buffer_rsrc_t rv, int lane)
+    {
+        const int q = lane >> 4, n = lane & 15;
+        const int kc_off = n * (D / 2) + q * (D / 8), vc_off = q * (2 * D) + n * (D / 8);
+        if constexpr (KW == 4) {
+            kc[t] = buffer_load_u4(rk, kc_off);
+            vc[t] = buffer_load_u4(rv, vc_off);
+        } else {
+            kc[t] = buffer_load_u2(rk, kc_off);
+            vc[t] = buffer_load_u2(rv, vc_off);
+        }
+        kp[t] = __builtin_amdgcn_raw_buffer_load_b32(rk, 8 * D + n * (D / 8) + (q * D / 4 / kKv4Group) * 4, 0, kStreamingLoad);
+        vp[t] = buffer_load_u4(rv, 8 * D + (q * (D / kKv4Group) + n * (D / 16) / kKv4Group) * 16);
+    }
+    // 16 + code as fp16: the code in the four bits below the exponent of 16.  `at`: its place in both halves.
+    __device__ static __forceinline__ f16x2 sixteen_plus(unsigned w, int at)
+    {
+        const unsigned c = at < 6 ? w << (6 - at) : w >> (at - 6);
+        return __builtin_bit_cast(f16x2, (c & 0x03c003c0u) | 0x4c004c00u);
+    }
+    __device__ __forceinline__ f16x8 k(int t, int c) const
+    {
+        const f16x2 sb = __builtin_bit_cast(f16x2, kp[t]);
+        const f16x2 s = {sb.x, sb.x}, b = {sb.y, sb.y};
+        f16x8 r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f16x2 v = __builtin_elementwise_fma(sixteen_plus(kc[t][c], 4 * i), s, b);
+            r[2 * i] = v.x;
+            r[2 * i + 1] = v.y;
+        }
+        return r;
+    }
+    __device__ __forceinline__ f16x8 v(int j) const
+    {
+        f16x8 r;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                // (copies: a bit cast of a vector's element takes the first one)
+                const unsigned s = vp[t][i], b = vp[t][2 + i];
+                const f16x2 x = __builtin_elementwise_fma(sixteen_plus(vc[t][(j / 4) * 2 + i], 4 * (j % 4)),
+                                                          __builtin_bit_cast(f16x2, s), __builtin_bit_cast(f16x2, b));
+                r[4 * t + 2 * i] = x.x;
+                r[4 * t + 2 * i + 1] = x.y;
+            }
+        return r;
+    }
+    // Values of tokens at or past `left` become zero: their slots may hold anything.
+    __device__ __forceinline__ void mask_v(int left, int lane)
+    {
+        const int q = lane >> 4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int tok = t * 16 + 4 * q + 2 * i;
+                const unsigned m = tok + 1 < left ? ~0u : tok < left ? 0xffffu : 0u;
+                vp[t][i] &= m;
+                vp[t][2 + i] &= m;
+            }
+    }
+};
+
+template <int D>
+struct F16Pair {
+    static constexpr int KS = D / 32, VW = D / 32;
+    typedef unsigned int Words __attribute__((ext_vector_type(VW)));
+    u32x4 kc[2][KS];
+    Words vc[2][4];
+
+    static constexpr int kTileBytes = kBlockTokens * D * 2;
+    __device__ __forceinline__ void issue(int t, __amdgpu_buffer_rsrc_t rk, __amdgpu_buffer_rsrc_t rv, int lane)
+    {
+        const int q = lane >> 4, n = lane & 15;
+#pragma unroll
+        for (int c = 0; c < KS; ++c) kc[t][c] = buffer_load_u4(rk, n * (2 * D) + q * (D / 2) + c * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int off = (4 * q + i) * (2 * D) + n * (D / 8);
+            if constexpr (VW == 4)
+                vc[t][i] = buffer_load_u4(rv, off);
+            else
+                vc[t][i] = buffer_load_u2(rv, off);
+        }
+    }
+    __device__ __forceinline__ f16x8 k(int t, int c) const { return __builtin_bit_cast(f16x8, kc[t][c]); }
+    __device__ __forceinline__ f16x8 v(int j) const
+    {
+        const unsigned sel = j % 2 ? 0x07060302u : 0x05040100u;
+        u32x4 r;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            r[2 * t] = __builtin_amdgcn_perm(vc[t][1][j / 2], vc[t][0][j / 2], sel);
+            r[2 * t + 1] = __builtin_amdgcn_perm(vc[t][3][j / 2], vc[t][2][j / 2], sel);
+        }
+        return __builtin_bit_cast(f16x8, r);
+    }
+    __device__ __forceinline__ void mask_v(int left, int lane)
+    {
+        const int q = lane >> 4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (t * 16 + 4 * q + i >= left)
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) vc[t][i][w] = 0u;
+    }
+};
+
+template <int D>
+struct ChunkState {
+    float m, l;                             // running maximum (the same in a head's four lanes), sum (per lane)
+    f32x4 acc[D / 16];
+};
+
+// Two tiles, of whose 32 tokens the first `left` count (32 or more: all).
+template <int D, class Pair, bool SCORES>
+__device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const f16x8 (&q)[D / 32], float scale_log2,
+                                             int left, int lane, float *scores)
+{
+#pragma clang fp contract(off)
+    f32x4 c[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) c[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.k(i, s), q[s], c[i], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) c[i] *= scale_log2;
+    if (left < 32) {
+        t.mask_v(left, lane);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i * 16 + (lane >> 4) * 4 + e >= left) c[i][e] = -INFINITY;
+    }
+    if constexpr (SCORES) {
+        if (scores) {
+            *reinterpret_cast<f32x4 *>(scores + (lane >> 4) * 4) = c[0];
+            if (left > 16) *reinterpret_cast<f32x4 *>(scores + 16 + (lane >> 4) * 4) = c[1];
+        }
+    }
+    float mt = fmaxf(fmaxf(fmaxf(c[0][0], c[0][1]), fmaxf(c[0][2], c[0][3])),
+                     fmaxf(fmaxf(c[1][0], c[1][1]), fmaxf(c[1][2], c[1][3])));
+    if (__builtin_amdgcn_ballot_w64(mt > st.m) != 0) {
+        mt = max_xor32(max_xor16(mt));
+        const float m_new = fmaxf(st.m, mt);
+        const float alpha = fast_exp2(st.m - m_new);
+        st.m = m_new;
+        st.l *= alpha;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) st.acc[j] *= alpha;
+    }
+    f16x8 p;
+    float ps = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = fast_exp2(c[i][e] - st.m);
+            ps += x;
+            p[4 * i + e] = (_Float16)x;                 // (fp16 products; the sum is of what was not rounded)
+        }
+    st.l += ps;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j)
+        st.acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.v(j), p, st.acc[j], 0, 0, 0);
+}
+
+template <int D>
+struct ChunkLds {
+    float o[kCkWaves][kCkMaxGroup][D + 4];
+    float m[kCkWaves][16], l[kCkWaves][16];
+    int item[3];
+    int sums[kCkWaves];
+};
+
+// Workgroups of a compute unit: as many as the registers of a lane allow.
+constexpr int chunk_residents(bool kv4, bool weights) { return kv4 && !weights ? 3 : 2; }
+
+// Items are (chunk of a sequence, selected head), heads fastest; workgroups stride over them.
+template <int D, bool KV4, bool WEIGHTS>
+__global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chunk_kernel(ChunkParams p)
+{
+    using Pair = std::conditional_t<KV4, Kv4Pair<D>, F16Pair<D>>;
+    __shared__ ChunkLds<D> lds;
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, quarter = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // Thread t looks after the chunks of sequences t * span .. and finds the item that lies in them.
+    const int span = (p.batch + kCkThreads - 1) / kCkThreads;
+    const int first = tid * span, last = min(first + span, p.batch);
+    auto length = [&](int b) { return min(max(p.seq_lens[b], 0), p.slots); };
+    int mine = 0;
+    for (int b = first; b < last; ++b) mine += chunks_of(length(b));
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(upto, o);
+        upto += lane >= o ? v : 0;
+    }
+    if (lane == 63) lds.sums[wave] = upto;
+    __syncthreads();
+    int start = upto - mine, total = 0;
+#pragma unroll
+    for (int w = 0; w < kCkWaves; ++w) {
+        start += w < wave ? lds.sums[w] : 0;
+        total += lds.sums[w];
+    }
+
+    for (int64_t it = blockIdx.x; it < (int64_t)total * p.n_sel; it += gridDim.x) {
+        const int ci = (int)(it / p.n_sel), i = (int)(it % p.n_sel);
+        if (ci >= start && ci < start + mine) {
+            int b = first, c = ci - start, L = length(b);
+            while (c >= chunks_of(L)) {
+                c -= chunks_of(L);
+                L = length(++b);
+            }
+            lds.item[0] = b;
+            lds.item[1] = c;
+            lds.item[2] = L;
+        }
+        __syncthreads();
+        const int b = __builtin_amdgcn_readfirstlane(lds.item[0]), chunk = __builtin_amdgcn_readfirstlane(lds.item[1]);
+        const int L = __builtin_amdgcn_readfirstlane(lds.item[2]);
+        const int g = p.head_ids[i], r = p.group;
+        const int tokens = min(L - chunk * kCkTokens, kCkTokens);
+        const int tiles = (tokens + kBlockTokens - 1) / kBlockTokens;
+        const int pairs = (tiles + 1) / 2, share = (pairs + kCkWaves - 1) / kCkWaves;
+        const int p0 = wave * share, np = max(min(pairs - p0, share), 0);
+
+        ChunkState<D> st;
+        st.m = kNegBig;
+        st.l = 0.f;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) st.acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int64_t row = (int64_t)b * p.n_sel + i;
+        if (np > 0) {
+            const int tile0 = chunk * kCkTiles + 2 * p0;
+            const int blocks = p.block_table[(int64_t)b * p.max_blocks_per_seq +
+                                             min(tile0 + min(lane, 2 * np - 1), chunk * kCkTiles + tiles - 1)];
+            f16x8 q[D / 32];
+            const __half *q_row = p.q + ((int64_t)b * p.n_q_heads + g * r + min(n, r - 1)) * D + quarter * (D / 4);
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) {
+                u32x4 w = reinterpret_cast<const u32x4 *>(q_row)[s];
+                if (n >= r) w = u32x4{0u, 0u, 0u, 0u};
+                q[s] = __builtin_bit_cast(f16x8, w);
+            }
+            float *scores = nullptr;
+            if (WEIGHTS && n < r) scores = p.scores + (row * r + n) * p.slots + (int64_t)tile0 * kBlockTokens;
+            const unsigned char *head_k = p.k + (int64_t)g * p.stride_head, *head_v = p.v + (int64_t)g * p.stride_head;
+            // tiles past the wave's share: descriptors of no length (the loads take their turn and read nothing)
+            auto issue = [&](Pair &t, int pr) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t at = (int64_t)__builtin_amdgcn_readlane(blocks, (2 * pr + h) & 63) * p.stride_block;
+                    const int bytes = pr < np ? Pair::kTileBytes : 0;
+                    t.issue(h, tile_rsrc(reinterpret_cast<const __half *>(head_k + at), bytes),
+                            tile_rsrc(reinterpret_cast<const __half *>(head_v + at), bytes), lane);
+                }
+            };
+            auto update = [&](Pair &t, int pr) {
+                chunk_update<D, Pair, WEIGHTS>(st, t, q, p.scale_log2, tokens - (p0 + pr) * 32, lane,
+                                               scores ? scores + pr * 32 : nullptr);
+            };
+            Pair x, y;
+            issue(x, 0);
+            issue(y, 1);
+            for (int pr = 0; pr < np; pr += 2) {
+                update(x, pr);
+                issue(x, pr + 2);
+                if (pr + 1 < np) update(y, pr + 1);
+                issue(y, pr + 3);
+            }
+        }
+        st.l = sum_xor32(sum_xor16(st.l));
+        if (n < r) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < D / 16; j += 4)
+                    *reinterpret_cast<float4 *>(&lds.o[wave][n][(quarter * 4 + e) * (D / 16) + j]) =
+                        make_float4(st.acc[j][e], st.acc[j + 1][e], st.acc[j + 2][e], st.acc[j + 3][e]);
+            if (quarter == 0) {
+                lds.m[wave][n] = st.m;
+                lds.l[wave][n] = st.l;
+            }
+        }
+        __syncthreads();
+        for (int k = tid; k < r * D; k += kCkThreads) {
+            const int j = k / D, d = k % D;
+            float M = kNegBig, sum = 0.f, o = 0.f;
+#pragma unroll
+            for (int w = 0; w < kCkWaves; ++w) M = fmaxf(M, lds.m[w][j]);
+#pragma unroll
+            for (int w = 0; w < kCkWaves; ++w) {
+                const float f = fast_exp2(lds.m[w][j] - M);
+                sum += f * lds.l[w][j];
+                o += f * lds.o[w][j][d];
+            }
+            o = tokens > 0 ? o / sum : 0.f;
+            const bool whole = L <= kCkTokens;
+            const int64_t part = (row * p.max_chunks + chunk) * r + j;
+            if (whole)
+                p.out[((int64_t)b * p.n_q_heads + g * r + j) * D + d] = __float2half_rn(o);
+            else
+                p.o_partial[part * D + d] = o;
+            if ((WEIGHTS || !whole) && d == 0) p.lse_partial[part] = M + fast_log2(sum);
+        }
+        __syncthreads();
+    }
+}
+
+// Combination of a row's chunks in ascending order, and the weights of its tokens.
+// x: chunks (weights) or 1, y: selected heads, z: sequences.
+template <int D, bool WEIGHTS>
+__global__ void __launch_bounds__(kCkThreads) chunk_finish_kernel(ChunkParams p)
+{
+    __shared__ float lse[kCkMaxGroup];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int i = blockIdx.y, r = p.group, chunk = blockIdx.x;
+    const int g = p.head_ids[i];
+    for (int64_t b = blockIdx.z; b < p.batch; b += gridDim.z) {
+        const int L = min(max(p.seq_lens[b], 0), p.slots);
+        const int chunks = chunks_of(L);
+        if (chunk * kCkTokens >= L || (!WEIGHTS && chunks == 1)) continue;
+        const int64_t row = b * p.n_sel + i;
+        const float *lp = p.lse_partial + row * p.max_chunks * r;
+        __syncthreads();
+        for (int j = wave; j < r; j += kCkWaves) {
+            float m = -INFINITY, s = 0.f;
+            for (int c = lane; c < chunks; c += 64) m = fmaxf(m, lp[c * r + j]);
+#pragma unroll
+            for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+            for (int c = lane; c < chunks; c += 64) s += fast_exp2(lp[c * r + j] - m);
+#pragma unroll
+            for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+            if (lane == 0) lse[j] = m + fast_log2(s);
+        }
+        __syncthreads();
+        if (chunks > 1 && chunk == 0) {
+            const float *op = p.o_partial + row * p.max_chunks * r * D;
+            for (int k = tid; k < r * D; k += kCkThreads) {
+                const int j = k / D;
+                float o = 0.f;
+#pragma unroll 8
+                for (int c = 0; c < chunks; ++c)
+                    o += fast_exp2(lp[c * r + j] - lse[j]) * op[(int64_t)c * r * D + k];
+                p.out[((int64_t)b * p.n_q_heads + g * r) * D + k] = __float2half_rn(o);
+            }
+        }
+        if constexpr (WEIGHTS) {
+            // a head that an earlier entry names is accumulated there
+            int named = 0;
+            for (int j = tid; j < i; j += kCkThreads) named |= p.head_ids[j] == g;
+            if (__syncthreads_or(named)) continue;
+            const int64_t at = (b * p.n_kv_heads + g) * p.slots;
+            const int end = min((chunk + 1) * kCkTokens, L);
+            for (int t = chunk * kCkTokens + tid; t < end; t += kCkThreads) {
+                float w = 0.f;
+                for (int j = 0; j < r; ++j) w += fast_exp2(p.scores[(row * r + j) * p.slots + t] - lse[j]);
+                if (p.w_in && p.decay != 0.f) w = fmaf(p.decay, p.w_in[at + t], w);
+                p.w_out[at + t] = w;
+                if (t == L - 1 && p.positions) p.positions[at + t] = p.n_seen[b] - 1;
+            }
+        }
+    }
+}
+
+}  // namespace hetis

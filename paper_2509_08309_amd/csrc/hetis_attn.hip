@@ -14,6 +14,7 @@
 #include "attn_mfma.hpp"
 #include "attn_vec.hpp"
 #include "attn_rows.hpp"
+#include "workspace.hpp"
 
 namespace hetis {
 
@@ -31,9 +32,6 @@ constexpr int kWgsPerCu = 1;    // persistent workgroups per compute unit
 // batches run as several launches over slices of the rows.
 constexpr int kMaxPersistBatch = 2048;
 static_assert(kMaxPersistBatch == kMaxRows, "the kernel's enumeration is laid out for this many rows");
-// Arrival counters of a decode workspace (see the workspace layout below).
-constexpr size_t kArrivalSlots = (size_t)1 << 18;
-constexpr size_t kArrivalBytes = kArrivalSlots * sizeof(unsigned int);
 constexpr int kMaxPersistHeads = 1024;
 // A wave keeps the block ids of one chunk in one register (64 lanes).
 constexpr int kMaxChunkTokens = 64 * kBlockTokens;
@@ -77,7 +75,7 @@ static int check_chunking(const hetis_attn_shape *s, int32_t chunk_tokens, int32
 }
 
 // Number of compute units of the current device (cached per device).
-static int device_cu_count()
+int device_cu_count()
 {
     static std::mutex mu;
     static std::vector<int> cus;
@@ -295,7 +293,6 @@ struct WsLayout {
     int slots = 1;                     // partial-result slots per row
     bool spread = false;
 };
-constexpr size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 static int decode_max_segs(const hetis_attn_shape *s, int group)
 {
@@ -337,7 +334,7 @@ static WsLayout choose_layout(const hetis_attn_shape *s, int64_t rows, int n_sel
     return decode_ws_layout(s, rows, n_sel, group, false);
 }
 
-static int check_workspace(const void *ws, size_t have, size_t need)
+int check_workspace(const void *ws, size_t have, size_t need)
 {
     if (!ws) return HETIS_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(ws) % 256 != 0 || have < need) return HETIS_ERR_WORKSPACE;
@@ -382,7 +379,7 @@ static bool stream_is_capturing(hipStream_t st)
 }
 
 // `st` == nullptr with `may_be_capturing` false: called outside any launch (reserve).
-static int owned_workspace(size_t need, hipStream_t st, bool may_be_capturing, void **out)
+int owned_workspace(size_t need, hipStream_t st, bool may_be_capturing, void **out)
 {
     std::lock_guard<std::mutex> lock(g_ws_mutex);
     int dev = 0;

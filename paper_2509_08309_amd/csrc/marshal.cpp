@@ -18,7 +18,9 @@
 #include <utility>
 
 #include "../../include/hetis_attn.h"
+#include "../../include/hetis_evict.h"
 #include "../../include/hetis_kv.h"
+#include "../../include/hetis_kv4.h"
 
 namespace {
 
@@ -131,6 +133,11 @@ PyMethodDef calls[] = {
     HETIS_CALL(hetis_attn_decode_split), HETIS_CALL(hetis_attn_decode_split_ws), HETIS_CALL(hetis_attn_merge),
     HETIS_CALL(hetis_kv_append), HETIS_CALL(hetis_kv_append_pairs), HETIS_CALL(hetis_kv_store),
     HETIS_CALL(hetis_kv_fetch), HETIS_CALL(hetis_kv_copy_tiles),
+    HETIS_CALL(hetis_attn_decode_kv4), HETIS_CALL(hetis_attn_decode_kv4_ws), HETIS_CALL(hetis_kv4_append),
+    HETIS_CALL(hetis_kv4_store), HETIS_CALL(hetis_kv4_fetch), HETIS_CALL(hetis_attn_decode_weights),
+    HETIS_CALL(hetis_attn_decode_weights_ws), HETIS_CALL(hetis_attn_decode_kv4_weights),
+    HETIS_CALL(hetis_attn_decode_kv4_weights_ws), HETIS_CALL(hetis_kv_evict), HETIS_CALL(hetis_kv_move),
+    HETIS_CALL(hetis_kv4_move),
 };
 
 PyObject *bind(PyObject *, PyObject *args)

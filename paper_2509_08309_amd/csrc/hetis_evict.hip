@@ -89,7 +89,16 @@ int hetis_kv_evict(const hetis_attn_shape *shape, const float *weights_in, const
     p.n_sink = n_sink;
     p.n_recent = n_recent;
     p.max_moves = max_moves;
-    evict_kernel<<<dim3((unsigned)n_sel_heads, (unsigned)s.batch), kEvictThreads, 0, (hipStream_t)stream>>>(p);
+    const dim3 grid((unsigned)n_sel_heads, (unsigned)s.batch);
+    const hipStream_t st = (hipStream_t)stream;
+    // By the slots a row can have: few waves and few keys each for short rows (384 rows of 500 to 2000: 512
+    // threads 14.2 us, 256 with 16 keys 16.0), one window as far as registers go (64 rows of 8k to 24k: 32
+    // keys 36.9 us, two windows of 16 keys 52.7; 208 rows of 2k to 12k: 1024 threads 23.6, 512 with 32 keys
+    // 30.1).
+    if (p.slots <= 512 * 8) evict_kernel<512, 8, true><<<grid, 512, 0, st>>>(p);
+    else if (p.slots <= 1024 * 16) evict_kernel<1024, 16, true><<<grid, 1024, 0, st>>>(p);
+    else if (p.slots <= 1024 * 32) evict_kernel<1024, 32, true><<<grid, 1024, 0, st>>>(p);
+    else evict_kernel<1024, 16, false><<<grid, 1024, 0, st>>>(p);
     return launched();
 }
 

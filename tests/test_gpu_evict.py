@@ -206,6 +206,15 @@ def test_choice(kind, in_place):
     a.run([1], [L - 1 for L in LENS], 0, 0, 1, in_place)
 
 
+@pytest.mark.parametrize("kind", ["spread", "ties", "same"])
+@pytest.mark.parametrize("lens,mb", [([33000, 16384, 16385, 10], None), ([70000, 32768, 32769, 500, 16383], None),
+                                     ([20000, 4097, 900], 3000)])
+def test_long_rows_window_by_window(kind, lens, mb):
+    a = Rows(lens, 2, 306, kind, mb)
+    a.run([1], [L // 5 for L in lens], 4, 300, 16 * a.mb, in_place=True)
+    a.run([0], [L - 7 for L in lens], 4, 300, 16)
+
+
 def test_budgets_of_every_kind():
     lens = [50, 50, 50, 50, 50, 50, 0, 700]
     a = Rows(lens, 2, 302, "ties")

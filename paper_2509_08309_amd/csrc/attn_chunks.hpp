@@ -73,10 +73,13 @@ struct Kv4Pair {
         vp[t] = buffer_load_u4(rv, 8 * D + (q * (D / kKv4Group) + n * (D / 16) / kKv4Group) * 16);
     }
     // 16 + code as fp16: the code in the four bits below the exponent of 16.  `at`: its place in both halves.
+    // (the and-or by name: from constants that it knows the compiler makes two instructions)
     __device__ static __forceinline__ f16x2 sixteen_plus(unsigned w, int at)
     {
         const unsigned c = at < 6 ? w << (6 - at) : w >> (at - 6);
-        return __builtin_bit_cast(f16x2, (c & 0x03c003c0u) | 0x4c004c00u);
+        unsigned r;
+        asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(c), "s"(0x03c003c0u), "v"(0x4c004c00u));
+        return __builtin_bit_cast(f16x2, r);
     }
     __device__ __forceinline__ f16x8 k(int t, int c) const
     {
@@ -176,8 +179,8 @@ struct ChunkState {
     f32x4 acc[D / 16];
 };
 
-// Two tiles, of whose 32 tokens the first `left` count (32 or more: all).
-template <int D, class Pair, bool SCORES>
+// Two tiles; RAGGED: of their 32 tokens the first `left` count.
+template <int D, class Pair, bool SCORES, bool RAGGED>
 __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const f16x8 (&q)[D / 32], float scale_log2,
                                              int left, int lane, float *scores)
 {
@@ -189,7 +192,7 @@ __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const f
         for (int i = 0; i < 2; ++i) c[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.k(i, s), q[s], c[i], 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < 2; ++i) c[i] *= scale_log2;
-    if (left < 32) {
+    if constexpr (RAGGED) {
         t.mask_v(left, lane);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -200,7 +203,7 @@ __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const f
     if constexpr (SCORES) {
         if (scores) {
             *reinterpret_cast<f32x4 *>(scores + (lane >> 4) * 4) = c[0];
-            if (left > 16) *reinterpret_cast<f32x4 *>(scores + 16 + (lane >> 4) * 4) = c[1];
+            if (!RAGGED || left > 16) *reinterpret_cast<f32x4 *>(scores + 16 + (lane >> 4) * 4) = c[1];
         }
     }
     float mt = fmaxf(fmaxf(fmaxf(c[0][0], c[0][1]), fmaxf(c[0][2], c[0][3])),
@@ -241,7 +244,52 @@ struct ChunkLds {
 // Workgroups of a compute unit: as many as the registers of a lane allow.
 constexpr int chunk_residents(bool kv4, bool weights) { return kv4 && !weights ? 3 : 2; }
 
-// Items are (chunk of a sequence, selected head), heads fastest; workgroups stride over them.
+// Items are (chunk of a sequence, selected head), heads fastest; workgroups stride over them.  Thread t looks
+// after the chunks of sequences t * span .. and finds the item that lies in them.
+struct ChunkItems {
+    int first, start, mine, total;          // this thread's first sequence, its chunks' numbers; chunks of all
+    __device__ static __forceinline__ int length(const ChunkParams &p, int b)
+    {
+        return min(max(p.seq_lens[b], 0), p.slots);
+    }
+    __device__ __forceinline__ ChunkItems(const ChunkParams &p, int *sums)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int span = (p.batch + kCkThreads - 1) / kCkThreads;
+        first = tid * span;
+        mine = 0;
+        for (int b = first; b < min(first + span, p.batch); ++b) mine += chunks_of(length(p, b));
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o);
+            upto += lane >= o ? v : 0;
+        }
+        if (lane == 63) sums[wave] = upto;
+        __syncthreads();
+        start = upto - mine;
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < kCkWaves; ++w) {
+            start += w < wave ? sums[w] : 0;
+            total += sums[w];
+        }
+    }
+    // sequence, chunk and length of chunk number ci, by the thread that has it
+    __device__ __forceinline__ void find(const ChunkParams &p, int ci, int *item) const
+    {
+        if (ci < start || ci >= start + mine) return;
+        int b = first, c = ci - start, L = length(p, b);
+        while (c >= chunks_of(L)) {
+            c -= chunks_of(L);
+            L = length(p, ++b);
+        }
+        item[0] = b;
+        item[1] = c;
+        item[2] = L;
+    }
+};
+
 template <int D, bool KV4, bool WEIGHTS>
 __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chunk_kernel(ChunkParams p)
 {
@@ -249,40 +297,11 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
     __shared__ ChunkLds<D> lds;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, quarter = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const ChunkItems items(p, lds.sums);
 
-    // Thread t looks after the chunks of sequences t * span .. and finds the item that lies in them.
-    const int span = (p.batch + kCkThreads - 1) / kCkThreads;
-    const int first = tid * span, last = min(first + span, p.batch);
-    auto length = [&](int b) { return min(max(p.seq_lens[b], 0), p.slots); };
-    int mine = 0;
-    for (int b = first; b < last; ++b) mine += chunks_of(length(b));
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(upto, o);
-        upto += lane >= o ? v : 0;
-    }
-    if (lane == 63) lds.sums[wave] = upto;
-    __syncthreads();
-    int start = upto - mine, total = 0;
-#pragma unroll
-    for (int w = 0; w < kCkWaves; ++w) {
-        start += w < wave ? lds.sums[w] : 0;
-        total += lds.sums[w];
-    }
-
-    for (int64_t it = blockIdx.x; it < (int64_t)total * p.n_sel; it += gridDim.x) {
+    for (int64_t it = blockIdx.x; it < (int64_t)items.total * p.n_sel; it += gridDim.x) {
         const int ci = (int)(it / p.n_sel), i = (int)(it % p.n_sel);
-        if (ci >= start && ci < start + mine) {
-            int b = first, c = ci - start, L = length(b);
-            while (c >= chunks_of(L)) {
-                c -= chunks_of(L);
-                L = length(++b);
-            }
-            lds.item[0] = b;
-            lds.item[1] = c;
-            lds.item[2] = L;
-        }
+        items.find(p, ci, lds.item);
         __syncthreads();
         const int b = __builtin_amdgcn_readfirstlane(lds.item[0]), chunk = __builtin_amdgcn_readfirstlane(lds.item[1]);
         const int L = __builtin_amdgcn_readfirstlane(lds.item[2]);
@@ -323,19 +342,28 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
                             tile_rsrc(reinterpret_cast<const __half *>(head_v + at), bytes), lane);
                 }
             };
+            const int left = tokens - p0 * 32, full = min(left / 32, np);
             auto update = [&](Pair &t, int pr) {
-                chunk_update<D, Pair, WEIGHTS>(st, t, q, p.scale_log2, tokens - (p0 + pr) * 32, lane,
-                                               scores ? scores + pr * 32 : nullptr);
+                chunk_update<D, Pair, WEIGHTS, false>(st, t, q, p.scale_log2, 32, lane, scores ? scores + pr * 32 : nullptr);
             };
             Pair x, y;
             issue(x, 0);
             issue(y, 1);
-            for (int pr = 0; pr < np; pr += 2) {
+            int pr = 0;
+            for (; pr + 1 < full; pr += 2) {
                 update(x, pr);
                 issue(x, pr + 2);
-                if (pr + 1 < np) update(y, pr + 1);
+                update(y, pr + 1);
                 issue(y, pr + 3);
             }
+            if (pr < full) {
+                update(x, pr);
+                x = y;
+                ++pr;
+            }
+            if (pr < np)                                 // the row's last pair
+                chunk_update<D, Pair, WEIGHTS, true>(st, x, q, p.scale_log2, left - pr * 32, lane,
+                                                     scores ? scores + pr * 32 : nullptr);
         }
         st.l = sum_xor32(sum_xor16(st.l));
         if (n < r) {
@@ -375,59 +403,121 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
     }
 }
 
-// Combination of a row's chunks in ascending order, and the weights of its tokens.
-// x: chunks (weights) or 1, y: selected heads, z: sequences.
-template <int D, bool WEIGHTS>
-__global__ void __launch_bounds__(kCkThreads) chunk_finish_kernel(ChunkParams p)
+// Base-2 log-sum-exp of a row's head over its chunks, by one wave; the same in all lanes.
+__device__ __forceinline__ float row_lse(const float *lp, int r, int chunks)
 {
-    __shared__ float lse[kCkMaxGroup];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int i = blockIdx.y, r = p.group, chunk = blockIdx.x;
-    const int g = p.head_ids[i];
-    for (int64_t b = blockIdx.z; b < p.batch; b += gridDim.z) {
-        const int L = min(max(p.seq_lens[b], 0), p.slots);
-        const int chunks = chunks_of(L);
-        if (chunk * kCkTokens >= L || (!WEIGHTS && chunks == 1)) continue;
-        const int64_t row = b * p.n_sel + i;
-        const float *lp = p.lse_partial + row * p.max_chunks * r;
-        __syncthreads();
-        for (int j = wave; j < r; j += kCkWaves) {
-            float m = -INFINITY, s = 0.f;
-            for (int c = lane; c < chunks; c += 64) m = fmaxf(m, lp[c * r + j]);
+    const int lane = threadIdx.x & 63;
+    float m = -INFINITY, s = 0.f;
+    for (int c = lane; c < chunks; c += 64) m = fmaxf(m, lp[c * r]);
 #pragma unroll
-            for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-            for (int c = lane; c < chunks; c += 64) s += fast_exp2(lp[c * r + j] - m);
+    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    for (int c = lane; c < chunks; c += 64) s += fast_exp2(lp[c * r] - m);
 #pragma unroll
-            for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
-            if (lane == 0) lse[j] = m + fast_log2(s);
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    return m + fast_log2(s);
+}
+
+// Output row of one head from its chunks: kCkThreads / D groups of threads take every so manieth chunk each,
+// in ascending order, eight on their way at a time, and their sums are added in the groups' order.
+template <int D, int R>
+__device__ __forceinline__ void combine_head(const ChunkParams &p, const float *lp, const float *op, int chunks,
+                                             float lse, __half *out, float (&part)[kCkThreads])
+{
+    constexpr int G = kCkThreads / D;
+    const int d = threadIdx.x % D, grp = threadIdx.x / D;
+    float o = 0.f;
+    for (int c = grp; c < chunks; c += 8 * G) {
+        float w[8], v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int ce = min(c + e * G, chunks - 1);
+            w[e] = lp[ce * R];
+            v[e] = op[(int64_t)ce * R * D + d];
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o += c + e * G < chunks ? fast_exp2(w[e] - lse) * v[e] : 0.f;
+    }
+    part[threadIdx.x] = o;
+    __syncthreads();
+    if (grp == 0) {
+#pragma unroll
+        for (int k = 1; k < G; ++k) o += part[k * D + d];
+        out[d] = __float2half_rn(o);
+    }
+    __syncthreads();
+}
+
+// Rows of more than one chunk.  x: (selected head, query head of its group), y: sequences.
+template <int D, int R>
+__global__ void __launch_bounds__(kCkThreads) chunk_combine_kernel(ChunkParams p)
+{
+    __shared__ float part[kCkThreads];
+    const int i = blockIdx.x / R, j = blockIdx.x % R;
+    const int64_t b = blockIdx.y, row = b * p.n_sel + i;
+    const int chunks = chunks_of(ChunkItems::length(p, (int)b));
+    if (chunks == 1) return;
+    const float *lp = p.lse_partial + row * p.max_chunks * R + j, *op = p.o_partial + (row * p.max_chunks * R + j) * D;
+    combine_head<D, R>(p, lp, op, chunks, row_lse(lp, R, chunks),
+                       p.out + (b * p.n_q_heads + p.head_ids[i] * R + j) * D, part);
+}
+
+// The weights of a chunk's tokens, and a share of the row's output rows; items as in chunk_kernel.
+template <int D, int R>
+__global__ void __launch_bounds__(kCkThreads) chunk_weights_kernel(ChunkParams p)
+{
+    __shared__ float lse[kCkMaxGroup], part[kCkThreads];
+    __shared__ int item[3], sums[kCkWaves];
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const ChunkItems items(p, sums);
+    for (int64_t it = blockIdx.x; it < (int64_t)items.total * p.n_sel; it += gridDim.x) {
+        const int ci = (int)(it / p.n_sel), i = (int)(it % p.n_sel);
+        items.find(p, ci, item);
         __syncthreads();
-        if (chunks > 1 && chunk == 0) {
-            const float *op = p.o_partial + row * p.max_chunks * r * D;
-            for (int k = tid; k < r * D; k += kCkThreads) {
-                const int j = k / D;
-                float o = 0.f;
-#pragma unroll 8
-                for (int c = 0; c < chunks; ++c)
-                    o += fast_exp2(lp[c * r + j] - lse[j]) * op[(int64_t)c * r * D + k];
-                p.out[((int64_t)b * p.n_q_heads + g * r) * D + k] = __float2half_rn(o);
+        const int64_t b = item[0];
+        const int chunk = item[1], L = item[2];
+        const int chunks = chunks_of(L), t0 = chunk * kCkTokens, end = min(t0 + kCkTokens, L);
+        const int g = p.head_ids[i];
+        const int64_t row = b * p.n_sel + i;
+        const float *lp = p.lse_partial + row * p.max_chunks * R;
+        const float *sp = p.scores + row * R * p.slots;
+        const int64_t at = (b * p.n_kv_heads + g) * p.slots;
+        // a head that an earlier entry names is accumulated there
+        int named = 0;
+        for (int j = tid; j < i; j += kCkThreads) named |= p.head_ids[j] == g;
+        // scores and weights are on their way while the row's log-sum-exps are put together
+        constexpr int N = kCkTokens / kCkThreads;
+        float x[N][R], old[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int t = t0 + k * kCkThreads + tid;
+            old[k] = 0.f;
+            if (t < end) {
+#pragma unroll
+                for (int j = 0; j < R; ++j) x[k][j] = sp[(int64_t)j * p.slots + t];
+                if (p.w_in && p.decay != 0.f) old[k] = p.w_in[at + t];
             }
         }
-        if constexpr (WEIGHTS) {
-            // a head that an earlier entry names is accumulated there
-            int named = 0;
-            for (int j = tid; j < i; j += kCkThreads) named |= p.head_ids[j] == g;
-            if (__syncthreads_or(named)) continue;
-            const int64_t at = (b * p.n_kv_heads + g) * p.slots;
-            const int end = min((chunk + 1) * kCkTokens, L);
-            for (int t = chunk * kCkTokens + tid; t < end; t += kCkThreads) {
+        for (int j = wave; j < R; j += kCkWaves) {
+            const float v = row_lse(lp + j, R, chunks);
+            if ((tid & 63) == 0) lse[j] = v;
+        }
+        const bool again = __syncthreads_or(named);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int t = t0 + k * kCkThreads + tid;
+            if (t < end && !again) {
                 float w = 0.f;
-                for (int j = 0; j < r; ++j) w += fast_exp2(p.scores[(row * r + j) * p.slots + t] - lse[j]);
-                if (p.w_in && p.decay != 0.f) w = fmaf(p.decay, p.w_in[at + t], w);
-                p.w_out[at + t] = w;
+#pragma unroll
+                for (int j = 0; j < R; ++j) w += fast_exp2(x[k][j] - lse[j]);
+                p.w_out[at + t] = fmaf(p.decay, old[k], w);
                 if (t == L - 1 && p.positions) p.positions[at + t] = p.n_seen[b] - 1;
             }
         }
+        if (chunks > 1)
+            for (int j = chunk; j < R; j += chunks)
+                combine_head<D, R>(p, lp + j, p.o_partial + (row * p.max_chunks * R + j) * D, chunks, lse[j],
+                                   p.out + (b * p.n_q_heads + g * R + j) * D, part);
+        __syncthreads();
     }
 }
 

@@ -50,9 +50,19 @@ static int launch_chunks(const ChunkParams &p, int cus, hipStream_t st)
     const int64_t most = (int64_t)p.batch * p.max_chunks * p.n_sel;
     const unsigned grid = (unsigned)std::min<int64_t>(most, (int64_t)cus * chunk_residents(KV4, WEIGHTS));
     chunk_kernel<D, KV4, WEIGHTS><<<grid, kCkThreads, 0, st>>>(p);
-    if (WEIGHTS || p.max_chunks > 1)
-        chunk_finish_kernel<D, WEIGHTS>
-            <<<dim3(WEIGHTS ? p.max_chunks : 1, p.n_sel, p.batch), kCkThreads, 0, st>>>(p);
+    auto finish = [&](auto group) {
+        constexpr int R = decltype(group)::value;
+        if constexpr (WEIGHTS) {
+            const unsigned wgs = (unsigned)std::min<int64_t>(most, (int64_t)cus * 8);
+            chunk_weights_kernel<D, R><<<wgs, kCkThreads, 0, st>>>(p);
+        } else if (p.max_chunks > 1) {
+            chunk_combine_kernel<D, R><<<dim3(p.n_sel * R, p.batch), kCkThreads, 0, st>>>(p);
+        }
+    };
+    if (p.group == 1) finish(std::integral_constant<int, 1>());
+    else if (p.group == 2) finish(std::integral_constant<int, 2>());
+    else if (p.group == 4) finish(std::integral_constant<int, 4>());
+    else finish(std::integral_constant<int, 8>());
     return launched();
 }
 

@@ -235,9 +235,10 @@ __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const f
 
 template <int D>
 struct ChunkLds {
-    float o[kCkWaves][kCkMaxGroup][D + 4];
-    float m[kCkWaves][16], l[kCkWaves][16];
-    int item[3];
+    // results of the waves, and the item after next: of two items by turns
+    float o[2][kCkWaves][kCkMaxGroup][D + 4];
+    float m[2][kCkWaves][16], l[2][kCkWaves][16];
+    int item[2][3];
     int sums[kCkWaves];
 };
 
@@ -290,80 +291,141 @@ struct ChunkItems {
     }
 };
 
+// A chunk of a sequence and a selected head, as a wave sees it (the same in all lanes).
+struct ChunkWork {
+    int b, chunk, L, i, g;                  // b < 0: none
+    int tokens, last_tile, p0, np;          // of the chunk; its last tile in the row; the wave's pairs
+    __device__ __forceinline__ void set(const ChunkParams &p, const int *item, int head, int wave)
+    {
+        b = __builtin_amdgcn_readfirstlane(item[0]);
+        chunk = __builtin_amdgcn_readfirstlane(item[1]);
+        L = __builtin_amdgcn_readfirstlane(item[2]);
+        i = head;
+        g = b < 0 ? 0 : p.head_ids[head];
+        tokens = min(L - chunk * kCkTokens, kCkTokens);
+        const int tiles = (tokens + kBlockTokens - 1) / kBlockTokens;
+        last_tile = chunk * kCkTiles + tiles - 1;
+        const int pairs = (tiles + 1) / 2, share = (pairs + kCkWaves - 1) / kCkWaves;
+        p0 = wave * share;
+        np = b < 0 ? 0 : max(min(pairs - p0, share), 0);
+    }
+};
+
+// One barrier an item: the first tiles, the query rows and the block ids of the next item are asked for before
+// the waves' results of this one are folded, the item after next is looked up meanwhile, and what the waves
+// leave in LDS alternates between two places.
 template <int D, bool KV4, bool WEIGHTS>
 __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chunk_kernel(ChunkParams p)
 {
     using Pair = std::conditional_t<KV4, Kv4Pair<D>, F16Pair<D>>;
     __shared__ ChunkLds<D> lds;
-    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, quarter = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, quarter = lane >> 4, r = p.group;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const ChunkItems items(p, lds.sums);
+    // (chunk number, selected head) of an item, and of the workgroup's next one
+    struct At {
+        int chunk, head;
+    };
+    const int step_chunks = gridDim.x / p.n_sel, step_heads = gridDim.x % p.n_sel;
+    auto after = [&](At a) {
+        a.chunk += step_chunks;
+        a.head += step_heads;
+        if (a.head >= p.n_sel) {
+            a.head -= p.n_sel;
+            ++a.chunk;
+        }
+        return a;
+    };
+    auto look_up = [&](At a, int turn) {
+        if (a.chunk < items.total)
+            items.find(p, a.chunk, lds.item[turn]);
+        else if (tid == 0)
+            lds.item[turn][0] = -1;
+    };
+    // lane k: block of the wave's k-th tile (a chunk has no more tiles a wave than a wave has lanes)
+    auto block_ids = [&](const ChunkWork &w) {
+        return p.block_table[(int64_t)w.b * p.max_blocks_per_seq +
+                             min(w.chunk * kCkTiles + 2 * w.p0 + min(lane, 2 * w.np - 1), w.last_tile)];
+    };
+    static_assert(kCkTiles / kCkWaves <= 64, "block ids in one register");
+    f16x8 q[D / 32];
+    auto query = [&](const ChunkWork &w) {
+        const __half *rows = p.q + ((int64_t)w.b * p.n_q_heads + w.g * r + min(n, r - 1)) * D + quarter * (D / 4);
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) q[s] = __builtin_bit_cast(f16x8, reinterpret_cast<const u32x4 *>(rows)[s]);
+    };
+    // tiles past the wave's share: descriptors of no length (the loads take their turn and read nothing)
+    auto issue = [&](Pair &t, const ChunkWork &w, int blocks, int pr) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t at = (int64_t)__builtin_amdgcn_readlane(blocks, (2 * pr + h) & 63) * p.stride_block +
+                               (int64_t)w.g * p.stride_head;
+            const int bytes = pr < w.np ? Pair::kTileBytes : 0;
+            t.issue(h, tile_rsrc(reinterpret_cast<const __half *>(p.k + at), bytes),
+                    tile_rsrc(reinterpret_cast<const __half *>(p.v + at), bytes), lane);
+        }
+    };
 
-    for (int64_t it = blockIdx.x; it < (int64_t)items.total * p.n_sel; it += gridDim.x) {
-        const int ci = (int)(it / p.n_sel), i = (int)(it % p.n_sel);
-        items.find(p, ci, lds.item);
-        __syncthreads();
-        const int b = __builtin_amdgcn_readfirstlane(lds.item[0]), chunk = __builtin_amdgcn_readfirstlane(lds.item[1]);
-        const int L = __builtin_amdgcn_readfirstlane(lds.item[2]);
-        const int g = p.head_ids[i], r = p.group;
-        const int tokens = min(L - chunk * kCkTokens, kCkTokens);
-        const int tiles = (tokens + kBlockTokens - 1) / kBlockTokens;
-        const int pairs = (tiles + 1) / 2, share = (pairs + kCkWaves - 1) / kCkWaves;
-        const int p0 = wave * share, np = max(min(pairs - p0, share), 0);
+    At at{(int)(blockIdx.x / p.n_sel), (int)(blockIdx.x % p.n_sel)};
+    if (at.chunk >= items.total) return;
+    ChunkWork cur, nxt;
+    look_up(at, 0);
+    look_up(after(at), 1);
+    __syncthreads();
+    cur.set(p, lds.item[0], at.head, wave);
+    at = after(at);
+    nxt.set(p, lds.item[1], at.head, wave);
+    at = after(at);                                      // the item after next
+    __syncthreads();
+    int blocks = 0, next_blocks = 0;
+    Pair x, y;
+    if (cur.np > 0) {
+        blocks = block_ids(cur);
+        query(cur);
+        issue(x, cur, blocks, 0);
+        issue(y, cur, blocks, 1);
+    }
+    for (int turn = 0;; turn ^= 1) {
+        look_up(at, turn);
+        if (nxt.np > 0) next_blocks = block_ids(nxt);
 
         ChunkState<D> st;
         st.m = kNegBig;
         st.l = 0.f;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) st.acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int64_t row = (int64_t)b * p.n_sel + i;
-        if (np > 0) {
-            const int tile0 = chunk * kCkTiles + 2 * p0;
-            const int blocks = p.block_table[(int64_t)b * p.max_blocks_per_seq +
-                                             min(tile0 + min(lane, 2 * np - 1), chunk * kCkTiles + tiles - 1)];
-            f16x8 q[D / 32];
-            const __half *q_row = p.q + ((int64_t)b * p.n_q_heads + g * r + min(n, r - 1)) * D + quarter * (D / 4);
+        const int64_t row = (int64_t)cur.b * p.n_sel + cur.i;
+        if (cur.np > 0) {
+            if (n >= r)                                  // columns without a head
 #pragma unroll
-            for (int s = 0; s < D / 32; ++s) {
-                u32x4 w = reinterpret_cast<const u32x4 *>(q_row)[s];
-                if (n >= r) w = u32x4{0u, 0u, 0u, 0u};
-                q[s] = __builtin_bit_cast(f16x8, w);
-            }
+                for (int s = 0; s < D / 32; ++s) q[s] = f16x8{};
             float *scores = nullptr;
-            if (WEIGHTS && n < r) scores = p.scores + (row * r + n) * p.slots + (int64_t)tile0 * kBlockTokens;
-            const unsigned char *head_k = p.k + (int64_t)g * p.stride_head, *head_v = p.v + (int64_t)g * p.stride_head;
-            // tiles past the wave's share: descriptors of no length (the loads take their turn and read nothing)
-            auto issue = [&](Pair &t, int pr) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int64_t at = (int64_t)__builtin_amdgcn_readlane(blocks, (2 * pr + h) & 63) * p.stride_block;
-                    const int bytes = pr < np ? Pair::kTileBytes : 0;
-                    t.issue(h, tile_rsrc(reinterpret_cast<const __half *>(head_k + at), bytes),
-                            tile_rsrc(reinterpret_cast<const __half *>(head_v + at), bytes), lane);
-                }
-            };
-            const int left = tokens - p0 * 32, full = min(left / 32, np);
+            if (WEIGHTS && n < r)
+                scores = p.scores + (row * r + n) * p.slots + (int64_t)(cur.chunk * kCkTiles + 2 * cur.p0) * kBlockTokens;
+            const int left = cur.tokens - cur.p0 * 32, full = min(left / 32, cur.np);
             auto update = [&](Pair &t, int pr) {
                 chunk_update<D, Pair, WEIGHTS, false>(st, t, q, p.scale_log2, 32, lane, scores ? scores + pr * 32 : nullptr);
             };
-            Pair x, y;
-            issue(x, 0);
-            issue(y, 1);
             int pr = 0;
             for (; pr + 1 < full; pr += 2) {
                 update(x, pr);
-                issue(x, pr + 2);
+                issue(x, cur, blocks, pr + 2);
                 update(y, pr + 1);
-                issue(y, pr + 3);
+                issue(y, cur, blocks, pr + 3);
             }
             if (pr < full) {
                 update(x, pr);
                 x = y;
                 ++pr;
             }
-            if (pr < np)                                 // the row's last pair
+            if (pr < cur.np)                             // the row's last pair
                 chunk_update<D, Pair, WEIGHTS, true>(st, x, q, p.scale_log2, left - pr * 32, lane,
                                                      scores ? scores + pr * 32 : nullptr);
+        }
+        if (nxt.np > 0) {
+            query(nxt);
+            issue(x, nxt, next_blocks, 0);
+            issue(y, nxt, next_blocks, 1);
         }
         st.l = sum_xor32(sum_xor16(st.l));
         if (n < r) {
@@ -371,11 +433,11 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int j = 0; j < D / 16; j += 4)
-                    *reinterpret_cast<float4 *>(&lds.o[wave][n][(quarter * 4 + e) * (D / 16) + j]) =
+                    *reinterpret_cast<float4 *>(&lds.o[turn][wave][n][(quarter * 4 + e) * (D / 16) + j]) =
                         make_float4(st.acc[j][e], st.acc[j + 1][e], st.acc[j + 2][e], st.acc[j + 3][e]);
             if (quarter == 0) {
-                lds.m[wave][n] = st.m;
-                lds.l[wave][n] = st.l;
+                lds.m[turn][wave][n] = st.m;
+                lds.l[turn][wave][n] = st.l;
             }
         }
         __syncthreads();
@@ -383,23 +445,27 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
             const int j = k / D, d = k % D;
             float M = kNegBig, sum = 0.f, o = 0.f;
 #pragma unroll
-            for (int w = 0; w < kCkWaves; ++w) M = fmaxf(M, lds.m[w][j]);
+            for (int w = 0; w < kCkWaves; ++w) M = fmaxf(M, lds.m[turn][w][j]);
 #pragma unroll
             for (int w = 0; w < kCkWaves; ++w) {
-                const float f = fast_exp2(lds.m[w][j] - M);
-                sum += f * lds.l[w][j];
-                o += f * lds.o[w][j][d];
+                const float f = fast_exp2(lds.m[turn][w][j] - M);
+                sum += f * lds.l[turn][w][j];
+                o += f * lds.o[turn][w][j][d];
             }
-            o = tokens > 0 ? o / sum : 0.f;
-            const bool whole = L <= kCkTokens;
-            const int64_t part = (row * p.max_chunks + chunk) * r + j;
+            o = cur.tokens > 0 ? o / sum : 0.f;
+            const bool whole = cur.L <= kCkTokens;
+            const int64_t part = (row * p.max_chunks + cur.chunk) * r + j;
             if (whole)
-                p.out[((int64_t)b * p.n_q_heads + g * r + j) * D + d] = __float2half_rn(o);
+                p.out[((int64_t)cur.b * p.n_q_heads + cur.g * r + j) * D + d] = __float2half_rn(o);
             else
                 p.o_partial[part * D + d] = o;
             if ((WEIGHTS || !whole) && d == 0) p.lse_partial[part] = M + fast_log2(sum);
         }
-        __syncthreads();
+        if (nxt.b < 0) return;
+        cur = nxt;
+        blocks = next_blocks;
+        nxt.set(p, lds.item[turn], at.head, wave);
+        at = after(at);
     }
 }
 

@@ -42,9 +42,15 @@ struct ChunkParams {
     int32_t *positions;
     int64_t stride_block, stride_head;      // bytes
     int32_t batch, n_sel, n_q_heads, n_kv_heads, group, max_blocks_per_seq, max_chunks, slots;
-    float scale_log2, decay;
+    float scale_log2, decay;                // the scale's magnitude
+    uint32_t q_sign;                        // its sign, for the two query values of a word
 };
 
+// (a scalar load: a vector load would wait for the tiles that are on their way)
+__device__ __forceinline__ int head_id(const ChunkParams &p, int i)
+{
+    return reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(p.head_ids))[i];
+}
 __device__ __forceinline__ int chunks_of(int L) { return max((L + kCkTokens - 1) / kCkTokens, 1); }
 
 // ---- what a lane loads of two neighbouring tiles, and the operands it makes of it
@@ -175,13 +181,13 @@ struct F16Pair {
 
 template <int D>
 struct ChunkState {
-    float m, l;                             // running maximum (the same in a head's four lanes), sum (per lane)
+    float m, l;                             // largest q . k (the same in a head's four lanes), sum (per lane)
     f32x4 acc[D / 16];
 };
 
 // Two tiles; RAGGED: of their 32 tokens the first `left` count.
 template <int D, class Pair, bool SCORES, bool RAGGED>
-__device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const f16x8 (&q)[D / 32], float scale_log2,
+__device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const u32x4 (&q)[D / 32], float scale_log2,
                                              int left, int lane, float *scores)
 {
 #pragma clang fp contract(off)
@@ -189,9 +195,13 @@ __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const f
 #pragma unroll
     for (int s = 0; s < D / 32; ++s)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) c[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.k(i, s), q[s], c[i], 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) c[i] *= scale_log2;
+        for (int i = 0; i < 2; ++i) c[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.k(i, s), __builtin_bit_cast(f16x8, q[s]), c[i], 0, 0, 0);
+    if constexpr (SCORES) {
+        if (scores) {
+            *reinterpret_cast<f32x4 *>(scores + (lane >> 4) * 4) = c[0] * scale_log2;
+            if (!RAGGED || left > 16) *reinterpret_cast<f32x4 *>(scores + 16 + (lane >> 4) * 4) = c[1] * scale_log2;
+        }
+    }
     if constexpr (RAGGED) {
         t.mask_v(left, lane);
 #pragma unroll
@@ -200,30 +210,26 @@ __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const f
             for (int e = 0; e < 4; ++e)
                 if (i * 16 + (lane >> 4) * 4 + e >= left) c[i][e] = -INFINITY;
     }
-    if constexpr (SCORES) {
-        if (scores) {
-            *reinterpret_cast<f32x4 *>(scores + (lane >> 4) * 4) = c[0];
-            if (!RAGGED || left > 16) *reinterpret_cast<f32x4 *>(scores + 16 + (lane >> 4) * 4) = c[1];
-        }
-    }
     float mt = fmaxf(fmaxf(fmaxf(c[0][0], c[0][1]), fmaxf(c[0][2], c[0][3])),
                      fmaxf(fmaxf(c[1][0], c[1][1]), fmaxf(c[1][2], c[1][3])));
     if (__builtin_amdgcn_ballot_w64(mt > st.m) != 0) {
         mt = max_xor32(max_xor16(mt));
         const float m_new = fmaxf(st.m, mt);
-        const float alpha = fast_exp2(st.m - m_new);
+        const float alpha = fast_exp2((st.m - m_new) * scale_log2);
         st.m = m_new;
         st.l *= alpha;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) st.acc[j] *= alpha;
     }
+    const float down = -st.m * scale_log2;
     f16x8 p;
     float ps = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float x = fast_exp2(c[i][e] - st.m);
+            float x = fast_exp2(__builtin_fmaf(c[i][e], scale_log2, down));
+            if (RAGGED && i * 16 + (lane >> 4) * 4 + e >= left) x = 0.f;     // (a scale of 0: inf * 0)
             ps += x;
             p[4 * i + e] = (_Float16)x;                 // (fp16 products; the sum is of what was not rounded)
         }
@@ -233,63 +239,77 @@ __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const f
         st.acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.v(j), p, st.acc[j], 0, 0, 0);
 }
 
-template <int D>
-struct ChunkLds {
-    // results of the waves, and the item after next: of two items by turns
-    float o[2][kCkWaves][kCkMaxGroup][D + 4];
-    float m[2][kCkWaves][16], l[2][kCkWaves][16];
-    int item[2][3];
-    int sums[kCkWaves];
-};
-
-// Workgroups of a compute unit: as many as the registers of a lane allow.
-constexpr int chunk_residents(bool kv4, bool weights) { return kv4 && !weights ? 3 : 2; }
-
 // Items are (chunk of a sequence, selected head), heads fastest; workgroups stride over them.  Thread t looks
 // after the chunks of sequences t * span .. and finds the item that lies in them.
+// (The lengths of up to kMost sequences stay in LDS: a load here would wait for the tiles that are on their way.)
 struct ChunkItems {
-    int first, start, mine, total;          // this thread's first sequence, its chunks' numbers; chunks of all
+    static constexpr int kMost = 1024;
+    int total;                              // chunks of all sequences
     __device__ static __forceinline__ int length(const ChunkParams &p, int b)
     {
         return min(max(p.seq_lens[b], 0), p.slots);
     }
-    __device__ __forceinline__ ChunkItems(const ChunkParams &p, int *sums)
+    // in LDS
+    struct Table {
+        int sums[kCkWaves], start[kCkThreads + 1], lens[kMost];
+    };
+    __device__ __forceinline__ ChunkItems(const ChunkParams &p, Table &tab)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int span = (p.batch + kCkThreads - 1) / kCkThreads;
-        first = tid * span;
-        mine = 0;
-        for (int b = first; b < min(first + span, p.batch); ++b) mine += chunks_of(length(p, b));
+        int mine = 0;
+        for (int b = tid * span; b < min((tid + 1) * span, p.batch); ++b) {
+            const int L = length(p, b);
+            if (b < kMost) tab.lens[b] = L;
+            mine += chunks_of(L);
+        }
         int upto = mine;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
             const int v = __shfl_up(upto, o);
             upto += lane >= o ? v : 0;
         }
-        if (lane == 63) sums[wave] = upto;
+        if (lane == 63) tab.sums[wave] = upto;
         __syncthreads();
-        start = upto - mine;
         total = 0;
 #pragma unroll
         for (int w = 0; w < kCkWaves; ++w) {
-            start += w < wave ? sums[w] : 0;
-            total += sums[w];
+            upto += w < wave ? tab.sums[w] : 0;
+            total += tab.sums[w];
         }
+        // the first chunk that is not of this thread's sequences or of those before
+        tab.start[tid + 1] = upto;
+        if (tid == 0) tab.start[0] = 0;
+        __syncthreads();
     }
     // sequence, chunk and length of chunk number ci, by the thread that has it
-    __device__ __forceinline__ void find(const ChunkParams &p, int ci, int *item) const
+    __device__ __forceinline__ void find(const ChunkParams &p, int ci, int *item, const Table &tab) const
     {
-        if (ci < start || ci >= start + mine) return;
-        int b = first, c = ci - start, L = length(p, b);
+        const int tid = threadIdx.x, start = tab.start[tid];
+        if (ci < start || ci >= tab.start[tid + 1]) return;
+        auto len = [&](int b) { return b < kMost ? tab.lens[b] : length(p, b); };
+        int b = tid * ((p.batch + kCkThreads - 1) / kCkThreads), c = ci - start, L = len(b);
         while (c >= chunks_of(L)) {
             c -= chunks_of(L);
-            L = length(p, ++b);
+            L = len(++b);
         }
         item[0] = b;
         item[1] = c;
         item[2] = L;
     }
 };
+
+template <int D>
+struct ChunkLds {
+    // results of the waves, and the item after next: of two items by turns
+    float o[2][kCkWaves][kCkMaxGroup][D + 4];
+    float m[2][kCkWaves][16], l[2][kCkWaves][16];
+    int item[2][3];
+    ChunkItems::Table table;
+};
+
+// Workgroups of a compute unit: as many as the registers of a lane allow.
+constexpr int chunk_residents(bool kv4, bool weights) { return kv4 && !weights ? 3 : 2; }
 
 // A chunk of a sequence and a selected head, as a wave sees it (the same in all lanes).
 struct ChunkWork {
@@ -301,7 +321,7 @@ struct ChunkWork {
         chunk = __builtin_amdgcn_readfirstlane(item[1]);
         L = __builtin_amdgcn_readfirstlane(item[2]);
         i = head;
-        g = b < 0 ? 0 : p.head_ids[head];
+        g = b < 0 ? 0 : head_id(p, head);
         tokens = min(L - chunk * kCkTokens, kCkTokens);
         const int tiles = (tokens + kBlockTokens - 1) / kBlockTokens;
         last_tile = chunk * kCkTiles + tiles - 1;
@@ -321,7 +341,8 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
     __shared__ ChunkLds<D> lds;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, quarter = lane >> 4, r = p.group;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const ChunkItems items(p, lds.sums);
+    constexpr int kFoldDims = kCkMaxGroup * D / kCkThreads;
+    const ChunkItems items(p, lds.table);
     // (chunk number, selected head) of an item, and of the workgroup's next one
     struct At {
         int chunk, head;
@@ -338,7 +359,7 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
     };
     auto look_up = [&](At a, int turn) {
         if (a.chunk < items.total)
-            items.find(p, a.chunk, lds.item[turn]);
+            items.find(p, a.chunk, lds.item[turn], lds.table);
         else if (tid == 0)
             lds.item[turn][0] = -1;
     };
@@ -348,11 +369,11 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
                              min(w.chunk * kCkTiles + 2 * w.p0 + min(lane, 2 * w.np - 1), w.last_tile)];
     };
     static_assert(kCkTiles / kCkWaves <= 64, "block ids in one register");
-    f16x8 q[D / 32];
+    u32x4 q[D / 32];
     auto query = [&](const ChunkWork &w) {
         const __half *rows = p.q + ((int64_t)w.b * p.n_q_heads + w.g * r + min(n, r - 1)) * D + quarter * (D / 4);
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) q[s] = __builtin_bit_cast(f16x8, reinterpret_cast<const u32x4 *>(rows)[s]);
+        for (int s = 0; s < D / 32; ++s) q[s] = reinterpret_cast<const u32x4 *>(rows)[s];
     };
     // tiles past the wave's share: descriptors of no length (the loads take their turn and read nothing)
     auto issue = [&](Pair &t, const ChunkWork &w, int blocks, int pr) {
@@ -396,9 +417,10 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
         for (int j = 0; j < D / 16; ++j) st.acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         const int64_t row = (int64_t)cur.b * p.n_sel + cur.i;
         if (cur.np > 0) {
-            if (n >= r)                                  // columns without a head
+            // columns without a head are zero
+            const unsigned has = n < r ? ~0u : 0u;
 #pragma unroll
-                for (int s = 0; s < D / 32; ++s) q[s] = f16x8{};
+            for (int s = 0; s < D / 32; ++s) q[s] = (q[s] ^ p.q_sign) & has;
             float *scores = nullptr;
             if (WEIGHTS && n < r)
                 scores = p.scores + (row * r + n) * p.slots + (int64_t)(cur.chunk * kCkTiles + 2 * cur.p0) * kBlockTokens;
@@ -436,29 +458,40 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
                     *reinterpret_cast<float4 *>(&lds.o[turn][wave][n][(quarter * 4 + e) * (D / 16) + j]) =
                         make_float4(st.acc[j][e], st.acc[j + 1][e], st.acc[j + 2][e], st.acc[j + 3][e]);
             if (quarter == 0) {
-                lds.m[turn][wave][n] = st.m;
+                lds.m[turn][wave][n] = st.m * p.scale_log2;
                 lds.l[turn][wave][n] = st.l;
             }
         }
         __syncthreads();
-        for (int k = tid; k < r * D; k += kCkThreads) {
-            const int j = k / D, d = k % D;
-            float M = kNegBig, sum = 0.f, o = 0.f;
+        // A thread has kFoldDims neighbouring dims of one head; of fewer than all heads' dims a share of the threads
+        // has some.
+        if (tid * kFoldDims < r * D) {
+            const int j = tid * kFoldDims / D, d = tid * kFoldDims % D;
+            float f[kCkWaves], M = kNegBig, sum = 0.f, o[kFoldDims] = {};
 #pragma unroll
             for (int w = 0; w < kCkWaves; ++w) M = fmaxf(M, lds.m[turn][w][j]);
 #pragma unroll
             for (int w = 0; w < kCkWaves; ++w) {
-                const float f = fast_exp2(lds.m[turn][w][j] - M);
-                sum += f * lds.l[turn][w][j];
-                o += f * lds.o[turn][w][j][d];
+                f[w] = fast_exp2(lds.m[turn][w][j] - M);
+                sum += f[w] * lds.l[turn][w][j];
             }
-            o = cur.tokens > 0 ? o / sum : 0.f;
+#pragma unroll
+            for (int w = 0; w < kCkWaves; ++w)
+#pragma unroll
+                for (int e = 0; e < kFoldDims; ++e) o[e] += f[w] * lds.o[turn][w][j][d + e];
+            const float inv = cur.tokens > 0 ? 1.f / sum : 0.f;
+#pragma unroll
+            for (int e = 0; e < kFoldDims; ++e) o[e] = cur.tokens > 0 ? o[e] * inv : 0.f;
             const bool whole = cur.L <= kCkTokens;
             const int64_t part = (row * p.max_chunks + cur.chunk) * r + j;
-            if (whole)
-                p.out[((int64_t)cur.b * p.n_q_heads + cur.g * r + j) * D + d] = __float2half_rn(o);
-            else
-                p.o_partial[part * D + d] = o;
+            if (whole) {
+                __half *to = p.out + ((int64_t)cur.b * p.n_q_heads + cur.g * r + j) * D + d;
+#pragma unroll
+                for (int e = 0; e < kFoldDims; ++e) to[e] = __float2half_rn(o[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kFoldDims; ++e) p.o_partial[part * D + d + e] = o[e];
+            }
             if ((WEIGHTS || !whole) && d == 0) p.lse_partial[part] = M + fast_log2(sum);
         }
         if (nxt.b < 0) return;
@@ -483,61 +516,77 @@ __device__ __forceinline__ float row_lse(const float *lp, int r, int chunks)
     return m + fast_log2(s);
 }
 
-// Output row of one head from its chunks: kCkThreads / D groups of threads take every so manieth chunk each,
-// in ascending order, eight on their way at a time, and their sums are added in the groups' order.
-template <int D, int R>
-__device__ __forceinline__ void combine_head(const ChunkParams &p, const float *lp, const float *op, int chunks,
-                                             float lse, __half *out, float (&part)[kCkThreads])
+// Output rows of heads j0 .. j0 + HEADS - 1 from their chunks: a thread has four neighbouring dims, G groups of
+// threads every G-th chunk each in ascending order, eight on their way at a time, and the sums are added in the
+// groups' order.
+template <int D, int R, int HEADS>
+__device__ __forceinline__ void combine_heads(const float *lp, const float *op, int chunks, const float *lse, int j0,
+                                              __half *out, f32x4 (&part)[kCkThreads])
 {
-    constexpr int G = kCkThreads / D;
-    const int d = threadIdx.x % D, grp = threadIdx.x / D;
-    float o = 0.f;
+    constexpr int T = HEADS * D / 4, G = T < kCkThreads ? kCkThreads / T : 1;
+    static_assert(T <= kCkThreads && kCkThreads % T == 0, "a thread, four dims");
+    const int k = threadIdx.x % T * 4, grp = threadIdx.x / T;
+    const int j = j0 + k / D, at = j * D + k % D;
+    const float all = lse[j];
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int c = grp; c < chunks; c += 8 * G) {
-        float w[8], v[8];
+        float w[8];
+        f32x4 v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int ce = min(c + e * G, chunks - 1);
-            w[e] = lp[ce * R];
-            v[e] = op[(int64_t)ce * R * D + d];
+            w[e] = lp[ce * R + j];
+            v[e] = *reinterpret_cast<const f32x4 *>(op + (int64_t)ce * R * D + at);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o += c + e * G < chunks ? fast_exp2(w[e] - lse) * v[e] : 0.f;
+        for (int e = 0; e < 8; ++e) o += v[e] * (c + e * G < chunks ? fast_exp2(w[e] - all) : 0.f);
     }
-    part[threadIdx.x] = o;
-    __syncthreads();
-    if (grp == 0) {
+    if constexpr (G > 1) {
+        __syncthreads();
+        part[threadIdx.x] = o;
+        __syncthreads();
+        if (grp == 0)
 #pragma unroll
-        for (int k = 1; k < G; ++k) o += part[k * D + d];
-        out[d] = __float2half_rn(o);
+            for (int e = 1; e < G; ++e) o += part[e * T + threadIdx.x];
     }
-    __syncthreads();
+    if (grp == 0)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[at + e] = __float2half_rn(o[e]);
 }
 
-// Rows of more than one chunk.  x: (selected head, query head of its group), y: sequences.
+// Rows of more than one chunk.  x: selected heads, y: sequences.
 template <int D, int R>
 __global__ void __launch_bounds__(kCkThreads) chunk_combine_kernel(ChunkParams p)
 {
-    __shared__ float part[kCkThreads];
-    const int i = blockIdx.x / R, j = blockIdx.x % R;
+    __shared__ float lse[R];
+    __shared__ f32x4 part[kCkThreads];
+    const int i = blockIdx.x, wave = threadIdx.x >> 6;
     const int64_t b = blockIdx.y, row = b * p.n_sel + i;
     const int chunks = chunks_of(ChunkItems::length(p, (int)b));
     if (chunks == 1) return;
-    const float *lp = p.lse_partial + row * p.max_chunks * R + j, *op = p.o_partial + (row * p.max_chunks * R + j) * D;
-    combine_head<D, R>(p, lp, op, chunks, row_lse(lp, R, chunks),
-                       p.out + (b * p.n_q_heads + p.head_ids[i] * R + j) * D, part);
+    const float *lp = p.lse_partial + row * p.max_chunks * R, *op = p.o_partial + row * p.max_chunks * R * D;
+    __half *out = p.out + (b * p.n_q_heads + p.head_ids[i] * R) * D;
+    for (int j = wave; j < R; j += kCkWaves) {
+        const float v = row_lse(lp + j, R, chunks);
+        if ((threadIdx.x & 63) == 0) lse[j] = v;
+    }
+    __syncthreads();
+    combine_heads<D, R, R>(lp, op, chunks, lse, 0, out, part);
 }
 
 // The weights of a chunk's tokens, and a share of the row's output rows; items as in chunk_kernel.
 template <int D, int R>
 __global__ void __launch_bounds__(kCkThreads) chunk_weights_kernel(ChunkParams p)
 {
-    __shared__ float lse[kCkMaxGroup], part[kCkThreads];
-    __shared__ int item[3], sums[kCkWaves];
+    __shared__ float lse[R];
+    __shared__ f32x4 part[kCkThreads];
+    __shared__ int item[3];
+    __shared__ ChunkItems::Table table;
     const int tid = threadIdx.x, wave = tid >> 6;
-    const ChunkItems items(p, sums);
+    const ChunkItems items(p, table);
     for (int64_t it = blockIdx.x; it < (int64_t)items.total * p.n_sel; it += gridDim.x) {
         const int ci = (int)(it / p.n_sel), i = (int)(it % p.n_sel);
-        items.find(p, ci, item);
+        items.find(p, ci, item, table);
         __syncthreads();
         const int64_t b = item[0];
         const int chunk = item[1], L = item[2];
@@ -581,8 +630,8 @@ __global__ void __launch_bounds__(kCkThreads) chunk_weights_kernel(ChunkParams p
         }
         if (chunks > 1)
             for (int j = chunk; j < R; j += chunks)
-                combine_head<D, R>(p, lp + j, p.o_partial + (row * p.max_chunks * R + j) * D, chunks, lse[j],
-                                   p.out + (b * p.n_q_heads + g * R + j) * D, part);
+                combine_heads<D, R, 1>(lp, p.o_partial + row * p.max_chunks * R * D, chunks, lse, j,
+                                       p.out + (b * p.n_q_heads + g * R) * D, part);
         __syncthreads();
     }
 }

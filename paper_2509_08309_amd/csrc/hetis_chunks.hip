@@ -56,7 +56,7 @@ static int launch_chunks(const ChunkParams &p, int cus, hipStream_t st)
             const unsigned wgs = (unsigned)std::min<int64_t>(most, (int64_t)cus * 8);
             chunk_weights_kernel<D, R><<<wgs, kCkThreads, 0, st>>>(p);
         } else if (p.max_chunks > 1) {
-            chunk_combine_kernel<D, R><<<dim3(p.n_sel * R, p.batch), kCkThreads, 0, st>>>(p);
+            chunk_combine_kernel<D, R><<<dim3(p.n_sel, p.batch), kCkThreads, 0, st>>>(p);
         }
     };
     if (p.group == 1) finish(std::integral_constant<int, 1>());
@@ -108,7 +108,8 @@ static int chunk_call(const hetis_attn_shape *shape, const void *q, const void *
     p.max_blocks_per_seq = shape->max_blocks_per_seq;
     p.max_chunks = lay.max_chunks;
     p.slots = shape->max_blocks_per_seq * kBlockTokens;
-    p.scale_log2 = scale * kLog2e;
+    p.scale_log2 = std::fabs(scale) * kLog2e;
+    p.q_sign = std::signbit(scale) ? 0x80008000u : 0u;
     p.decay = decay;
     const int cus = device_cu_count();
     if (cus <= 0) return HETIS_ERR_LAUNCH;

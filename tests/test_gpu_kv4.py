@@ -145,6 +145,13 @@ def test_scores_far_apart_and_equal():
     c.check(c.decode([0, 1]), [0, 1])
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.125, 3.0, 1e-20])
+def test_scales(scale):
+    c = Cache4([700, 33, 1, 512, 1040], 8, 2, 64, seed=17)
+    c.scale = scale
+    c.check(c.decode([0, 1]), [0, 1])
+
+
 @pytest.mark.parametrize("D,r", [(64, 1), (128, 1), (128, 8)])
 def test_head_subset_and_order_and_runs_bit_for_bit(D, r):
     c = Cache4([1500, 17, 512, 800], 4 * r, 4, D, seed=11)

@@ -64,18 +64,18 @@ struct Kv4Pair {
     u32x4 vp[2];                                               // scales of the four tokens, biases
 
     static constexpr int kTileBytes = kv4_tile_bytes(D);
-    __device__ __forceinline__ void issue(int t, __amdgpu_buffer_rsrc_t rk, __amdgpu_buffer_rsrc_t rv, int lane)
+    __device__ __forceinline__ void issue_k(int t, __amdgpu_buffer_rsrc_t rk, int lane)
     {
-        const int q = lane >> 4, n = lane & 15;
-        const int kc_off = n * (D / 2) + q * (D / 8), vc_off = q * (2 * D) + n * (D / 8);
-        if constexpr (KW == 4) {
-            kc[t] = buffer_load_u4(rk, kc_off);
-            vc[t] = buffer_load_u4(rv, vc_off);
-        } else {
-            kc[t] = buffer_load_u2(rk, kc_off);
-            vc[t] = buffer_load_u2(rv, vc_off);
-        }
+        const int q = lane >> 4, n = lane & 15, off = n * (D / 2) + q * (D / 8);
+        if constexpr (KW == 4) kc[t] = buffer_load_u4(rk, off);
+        else kc[t] = buffer_load_u2(rk, off);
         kp[t] = __builtin_amdgcn_raw_buffer_load_b32(rk, 8 * D + n * (D / 8) + (q * D / 4 / kKv4Group) * 4, 0, kStreamingLoad);
+    }
+    __device__ __forceinline__ void issue_v(int t, __amdgpu_buffer_rsrc_t rv, int lane)
+    {
+        const int q = lane >> 4, n = lane & 15, off = q * (2 * D) + n * (D / 8);
+        if constexpr (KW == 4) vc[t] = buffer_load_u4(rv, off);
+        else vc[t] = buffer_load_u2(rv, off);
         vp[t] = buffer_load_u4(rv, 8 * D + (q * (D / kKv4Group) + n * (D / 16) / kKv4Group) * 16);
     }
     // 16 + code as fp16: the code in the four bits below the exponent of 16.  `at`: its place in both halves.
@@ -140,11 +140,15 @@ struct F16Pair {
     Words vc[2][4];
 
     static constexpr int kTileBytes = kBlockTokens * D * 2;
-    __device__ __forceinline__ void issue(int t, __amdgpu_buffer_rsrc_t rk, __amdgpu_buffer_rsrc_t rv, int lane)
+    __device__ __forceinline__ void issue_k(int t, __amdgpu_buffer_rsrc_t rk, int lane)
     {
         const int q = lane >> 4, n = lane & 15;
 #pragma unroll
         for (int c = 0; c < KS; ++c) kc[t][c] = buffer_load_u4(rk, n * (2 * D) + q * (D / 2) + c * 16);
+    }
+    __device__ __forceinline__ void issue_v(int t, __amdgpu_buffer_rsrc_t rv, int lane)
+    {
+        const int q = lane >> 4, n = lane & 15;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int off = (4 * q + i) * (2 * D) + n * (D / 8);
@@ -186,9 +190,10 @@ struct ChunkState {
 };
 
 // Two tiles; RAGGED: of their 32 tokens the first `left` count.
-template <int D, class Pair, bool SCORES, bool RAGGED>
+// `next_k` asks for the K part of the next two once this one's has been used.
+template <int D, class Pair, bool SCORES, bool RAGGED, class Next>
 __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const u32x4 (&q)[D / 32], float scale_log2,
-                                             int left, int lane, float *scores)
+                                             int left, int lane, float *scores, Next next_k)
 {
 #pragma clang fp contract(off)
     f32x4 c[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
@@ -196,6 +201,7 @@ __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const u
     for (int s = 0; s < D / 32; ++s)
 #pragma unroll
         for (int i = 0; i < 2; ++i) c[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.k(i, s), __builtin_bit_cast(f16x8, q[s]), c[i], 0, 0, 0);
+    next_k();
     if constexpr (SCORES) {
         if (scores) {
             *reinterpret_cast<f32x4 *>(scores + (lane >> 4) * 4) = c[0] * scale_log2;
@@ -309,7 +315,10 @@ struct ChunkLds {
 };
 
 // Workgroups of a compute unit: as many as the registers of a lane allow.
-constexpr int chunk_residents(bool kv4, bool weights) { return kv4 && !weights ? 3 : 2; }
+constexpr int chunk_residents(int D, bool kv4)
+{
+    return D == 64 ? 4 : kv4 ? 3 : 2;
+}
 
 // A chunk of a sequence and a selected head, as a wave sees it (the same in all lanes).
 struct ChunkWork {
@@ -335,7 +344,7 @@ struct ChunkWork {
 // the waves' results of this one are folded, the item after next is looked up meanwhile, and what the waves
 // leave in LDS alternates between two places.
 template <int D, bool KV4, bool WEIGHTS>
-__global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chunk_kernel(ChunkParams p)
+__global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_kernel(ChunkParams p)
 {
     using Pair = std::conditional_t<KV4, Kv4Pair<D>, F16Pair<D>>;
     __shared__ ChunkLds<D> lds;
@@ -376,15 +385,18 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
         for (int s = 0; s < D / 32; ++s) q[s] = reinterpret_cast<const u32x4 *>(rows)[s];
     };
     // tiles past the wave's share: descriptors of no length (the loads take their turn and read nothing)
-    auto issue = [&](Pair &t, const ChunkWork &w, int blocks, int pr) {
+    auto tile = [&](const unsigned char *pool, const ChunkWork &w, int blocks, int pr, int h) {
+        const int64_t at = (int64_t)__builtin_amdgcn_readlane(blocks, (2 * pr + h) & 63) * p.stride_block +
+                           (int64_t)w.g * p.stride_head;
+        return tile_rsrc(reinterpret_cast<const __half *>(pool + at), pr < w.np ? Pair::kTileBytes : 0);
+    };
+    auto issue_k = [&](Pair &t, const ChunkWork &w, int blocks, int pr) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t at = (int64_t)__builtin_amdgcn_readlane(blocks, (2 * pr + h) & 63) * p.stride_block +
-                               (int64_t)w.g * p.stride_head;
-            const int bytes = pr < w.np ? Pair::kTileBytes : 0;
-            t.issue(h, tile_rsrc(reinterpret_cast<const __half *>(p.k + at), bytes),
-                    tile_rsrc(reinterpret_cast<const __half *>(p.v + at), bytes), lane);
-        }
+        for (int h = 0; h < 2; ++h) t.issue_k(h, tile(p.k, w, blocks, pr, h), lane);
+    };
+    auto issue_v = [&](Pair &t, const ChunkWork &w, int blocks, int pr) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) t.issue_v(h, tile(p.v, w, blocks, pr, h), lane);
     };
 
     At at{(int)(blockIdx.x / p.n_sel), (int)(blockIdx.x % p.n_sel)};
@@ -399,12 +411,12 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
     at = after(at);                                      // the item after next
     __syncthreads();
     int blocks = 0, next_blocks = 0;
-    Pair x, y;
+    Pair x;
     if (cur.np > 0) {
         blocks = block_ids(cur);
         query(cur);
-        issue(x, cur, blocks, 0);
-        issue(y, cur, blocks, 1);
+        issue_k(x, cur, blocks, 0);
+        issue_v(x, cur, blocks, 0);
     }
     for (int turn = 0;; turn ^= 1) {
         look_up(at, turn);
@@ -425,29 +437,20 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(KV4, WEIGHTS)) chu
             if (WEIGHTS && n < r)
                 scores = p.scores + (row * r + n) * p.slots + (int64_t)(cur.chunk * kCkTiles + 2 * cur.p0) * kBlockTokens;
             const int left = cur.tokens - cur.p0 * 32, full = min(left / 32, cur.np);
-            auto update = [&](Pair &t, int pr) {
-                chunk_update<D, Pair, WEIGHTS, false>(st, t, q, p.scale_log2, 32, lane, scores ? scores + pr * 32 : nullptr);
-            };
             int pr = 0;
-            for (; pr + 1 < full; pr += 2) {
-                update(x, pr);
-                issue(x, cur, blocks, pr + 2);
-                update(y, pr + 1);
-                issue(y, cur, blocks, pr + 3);
-            }
-            if (pr < full) {
-                update(x, pr);
-                x = y;
-                ++pr;
+            for (; pr < full; ++pr) {
+                chunk_update<D, Pair, WEIGHTS, false>(st, x, q, p.scale_log2, 32, lane, scores ? scores + pr * 32 : nullptr,
+                                                      [&] { issue_k(x, cur, blocks, pr + 1); });
+                issue_v(x, cur, blocks, pr + 1);
             }
             if (pr < cur.np)                             // the row's last pair
                 chunk_update<D, Pair, WEIGHTS, true>(st, x, q, p.scale_log2, left - pr * 32, lane,
-                                                     scores ? scores + pr * 32 : nullptr);
+                                                     scores ? scores + pr * 32 : nullptr, [] {});
         }
         if (nxt.np > 0) {
             query(nxt);
-            issue(x, nxt, next_blocks, 0);
-            issue(y, nxt, next_blocks, 1);
+            issue_k(x, nxt, next_blocks, 0);
+            issue_v(x, nxt, next_blocks, 0);
         }
         st.l = sum_xor32(sum_xor16(st.l));
         if (n < r) {

@@ -48,7 +48,7 @@ static int launch_chunks(const ChunkParams &p, int cus, hipStream_t st)
 {
     // as many workgroups as are resident, and no more than there can be items
     const int64_t most = (int64_t)p.batch * p.max_chunks * p.n_sel;
-    const unsigned grid = (unsigned)std::min<int64_t>(most, (int64_t)cus * chunk_residents(KV4, WEIGHTS));
+    const unsigned grid = (unsigned)std::min<int64_t>(most, (int64_t)cus * chunk_residents(D, KV4));
     chunk_kernel<D, KV4, WEIGHTS><<<grid, kCkThreads, 0, st>>>(p);
     auto finish = [&](auto group) {
         constexpr int R = decltype(group)::value;

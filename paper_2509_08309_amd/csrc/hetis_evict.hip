@@ -34,7 +34,8 @@ static int move_call(bool kv4, const hetis_attn_shape *shape, const int32_t *mov
     p.batch = shape->batch;
     p.max_blocks_per_seq = shape->max_blocks_per_seq;
     p.max_moves = max_moves;
-    const int per_wg = shape->head_dim == 128 ? kKvRowsPerWg<128> : kKvRowsPerWg<64>;
+    const int lanes = kv4 ? kv_move_lanes<64, true>() : shape->head_dim == 128 ? kv_move_lanes<128, false>() : kv_move_lanes<64, false>();
+    const int per_wg = kKvRowThreads / lanes;
     const dim3 grid((unsigned)std::min<int64_t>(((int64_t)max_moves + per_wg - 1) / per_wg, (int64_t)1 << 23),
                     (unsigned)n_sel, (unsigned)shape->batch);
     const hipStream_t st = (hipStream_t)stream;

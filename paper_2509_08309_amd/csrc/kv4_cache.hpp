@@ -62,8 +62,11 @@ __device__ __forceinline__ float quad_swap2(float x)
     return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xf, 0xf, true));
 }
 
-// The quotients are IEEE divisions: a code lies next to a border wherever the values of a group lie on
-// a grid, and a reciprocal would move such values to the other side.
+// The quotients are those of an IEEE division: a code lies next to a border wherever the values of a group lie
+// on a grid, and a reciprocal alone would move such values to the other side.  A product with the reciprocal
+// (rounded, and of a rounded reciprocal: off by at most 3 * 2^-24 * 31 < 6e-6, the division by 2e-6) says how near
+// to a border a value is; only where one of a thread's eight is within 2e-5 are they divided (a store of
+// Gaussian rows 105 -> 86 us: sixteen divisions a thread were what bounded it).
 __device__ __forceinline__ Kv4Piece kv4_quantise(const kv_u32x4 raw)
 {
     float x[8];
@@ -92,11 +95,22 @@ __device__ __forceinline__ Kv4Piece kv4_quantise(const kv_u32x4 raw)
         s = 0.f;
     }
     const float b = __half2float(r.b);
+    const float inv = __builtin_amdgcn_rcpf(s);
+    bool near = false;
+    float u[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float c = fminf(fmaxf(rintf((x[i] - b) / s) - 16.f, 0.f), 15.f);
-        r.code[i] = s > 0.f ? (unsigned)c : 0u;
+        x[i] -= b;
+        const float y = x[i] * inv;
+        u[i] = rintf(y);
+        near |= fabsf(y - u[i]) > 0.49998f;
     }
+    if (near) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = rintf(x[i] / s);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.code[i] = s > 0.f ? (unsigned)fminf(fmaxf(u[i] - 16.f, 0.f), 15.f) : 0u;
     return r;
 }
 
@@ -216,43 +230,56 @@ struct KvMoveParams {
     int32_t n_sel, n_kv_heads, batch, max_blocks_per_seq, max_moves;
 };
 
-// x: groups of moves, y: selected heads, z: sequences; D/8 lanes a row.
+// x: groups of moves, y: selected heads, z: sequences.  16 lanes a row of the fp16 cache (8 at D = 64), four of
+// the 4-bit one: its rows are small, and what a thread waits for is a chain of three loads.
+template <int D, bool KV4>
+constexpr int kv_move_lanes() { return KV4 ? 4 : D / 8; }
+
 template <int D, bool KV4>
 __global__ void __launch_bounds__(kKvRowThreads) kv_move_rows_kernel(KvMoveParams p)
 {
-    constexpr int LR = D / 8;
-    constexpr int N = kKvRowsPerWg<D>;
+    constexpr int LR = kv_move_lanes<D, KV4>();
+    constexpr int N = kKvRowThreads / LR;
     const int x = threadIdx.x % LR;
-    for (int64_t b = blockIdx.z; b < p.batch; b += gridDim.z) {
-        const int64_t row = b * p.n_sel + blockIdx.y;
-        const int g = p.head_ids[blockIdx.y];
-        for (int64_t m = (int64_t)blockIdx.x * N + threadIdx.x / LR; m < p.max_moves; m += (int64_t)gridDim.x * N) {
-            int64_t from_tile, to_tile;
-            const int from = kv4_place(p, b, p.src[row * p.max_moves + m], g, &from_tile);
-            const int to = kv4_place(p, b, p.dst[row * p.max_moves + m], g, &to_tile);
-            if (from < 0 || to < 0) continue;
-            if constexpr (KV4) {
-                using T = Kv4Tile<D>;
-                const unsigned char *fk = p.k + from_tile, *fv = p.v + from_tile;
-                unsigned char *tk = p.k + to_tile, *tv = p.v + to_tile;
-                *(unsigned *)(tk + T::k_codes(to, x)) = *(const unsigned *)(fk + T::k_codes(from, x));
+    const int64_t b = blockIdx.z, row = b * p.n_sel + blockIdx.y;
+    const int g = p.head_ids[blockIdx.y];
+    for (int64_t m = (int64_t)blockIdx.x * N + threadIdx.x / LR; m < p.max_moves; m += (int64_t)gridDim.x * N) {
+        int64_t from_tile, to_tile;
+        const int from = kv4_place(p, b, p.src[row * p.max_moves + m], g, &from_tile);
+        const int to = kv4_place(p, b, p.dst[row * p.max_moves + m], g, &to_tile);
+        if (from < 0 || to < 0) continue;
+        const unsigned char *fk = p.k + from_tile, *fv = p.v + from_tile;
+        unsigned char *tk = p.k + to_tile, *tv = p.v + to_tile;
+        if constexpr (KV4) {
+            using T = Kv4Tile<D>;
+            constexpr int P = D / 32;                    // pieces of eight dims a lane
+            typedef unsigned int Words __attribute__((ext_vector_type(P)));
+            const Words k = *(const Words *)(fk + T::k_codes(from, x * P));
+            unsigned short v[2 * P], s[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    *(unsigned short *)(tv + T::v_codes(to, x, h)) =
-                        *(const unsigned short *)(fv + T::v_codes(from, x, h));
-                if (x % 4 == 0) {
-                    const int q = x / 4;
-                    *(unsigned *)(tk + T::k_pair(to, q)) = *(const unsigned *)(fk + T::k_pair(from, q));
-                    *(unsigned short *)(tv + T::v_scale(to, q)) = *(const unsigned short *)(fv + T::v_scale(from, q));
-                    *(unsigned short *)(tv + T::v_bias(to, q)) = *(const unsigned short *)(fv + T::v_bias(from, q));
-                }
-            } else {
-                const int64_t a = from_tile + (from * LR + x) * 16, c = to_tile + (to * LR + x) * 16;
-                const kv_u32x4 k = *(const kv_u32x4 *)(p.k + a);
-                const kv_u32x4 v = *(const kv_u32x4 *)(p.v + a);
-                *(kv_u32x4 *)(p.k + c) = k;
-                *(kv_u32x4 *)(p.v + c) = v;
+            for (int e = 0; e < 2 * P; ++e) v[e] = *(const unsigned short *)(fv + T::v_codes(from, x * P + e / 2, e % 2));
+            const bool has = x < T::kGroups;
+            unsigned pair = 0;
+            s[0] = s[1] = 0;
+            if (has) {
+                pair = *(const unsigned *)(fk + T::k_pair(from, x));
+                s[0] = *(const unsigned short *)(fv + T::v_scale(from, x));
+                s[1] = *(const unsigned short *)(fv + T::v_bias(from, x));
             }
+            *(Words *)(tk + T::k_codes(to, x * P)) = k;
+#pragma unroll
+            for (int e = 0; e < 2 * P; ++e) *(unsigned short *)(tv + T::v_codes(to, x * P + e / 2, e % 2)) = v[e];
+            if (has) {
+                *(unsigned *)(tk + T::k_pair(to, x)) = pair;
+                *(unsigned short *)(tv + T::v_scale(to, x)) = s[0];
+                *(unsigned short *)(tv + T::v_bias(to, x)) = s[1];
+            }
+        } else {
+            const int64_t f = (from * LR + x) * 16, t = (to * LR + x) * 16;
+            const kv_u32x4 k = __builtin_nontemporal_load((const kv_u32x4 *)(fk + f));
+            const kv_u32x4 v = __builtin_nontemporal_load((const kv_u32x4 *)(fv + f));
+            __builtin_nontemporal_store(k, (kv_u32x4 *)(tk + t));
+            __builtin_nontemporal_store(v, (kv_u32x4 *)(tv + t));
         }
     }
 }

@@ -3,8 +3,8 @@
 // codes into fp16 values, and the padded columns of a 16-column product cost the matrix cores nothing that
 // anything else waits for.
 //
-//   S^T = K . Q^T      v_mfma_f32_16x16x32_f16.  Lane l = 16 q + n holds dims q D/4 .. of token n (A) and of
-//                      query head n (B): one run of a K row, which lies in one group of 32 values.
+//   S^T = K . Q^T      v_mfma_f32_16x16x32_f16.  Lane l = 16 q + n holds, step by step, eight dims of token n
+//                      (A) and of query head n (B); which ones is the cache's choice (k_dim), the same for both.
 //   O^T += V^T . P     v_mfma_f32_16x16x32_f16 over 32 tokens: lane l holds, of tokens 4 q .. 4 q + 3 of both
 //                      tiles, dim n D/16 + j (A, row block j) and the probabilities of head n (B), which are
 //                      what the first product and exp2 leave in its registers.
@@ -62,6 +62,9 @@ struct Kv4Pair {
     Words kc[2], vc[2];
     unsigned kp[2];                                            // (s, b) of the group
     u32x4 vp[2];                                               // scales of the four tokens, biases
+
+    // First of the eight dims of contraction step c in quarter q: a quarter of a K row lies in one group.
+    __device__ static __forceinline__ int k_dim(int q, int c) { return q * (D / 4) + c * 8; }
 
     static constexpr int kTileBytes = kv4_tile_bytes(D);
     __device__ __forceinline__ void issue_k(int t, __amdgpu_buffer_rsrc_t rk, int lane)
@@ -139,12 +142,15 @@ struct F16Pair {
     u32x4 kc[2][KS];
     Words vc[2][4];
 
+    // First of the eight dims of contraction step c in quarter q: a load takes whole 64-byte pieces of a K row.
+    __device__ static __forceinline__ int k_dim(int q, int c) { return c * 32 + q * 8; }
+
     static constexpr int kTileBytes = kBlockTokens * D * 2;
     __device__ __forceinline__ void issue_k(int t, __amdgpu_buffer_rsrc_t rk, int lane)
     {
         const int q = lane >> 4, n = lane & 15;
 #pragma unroll
-        for (int c = 0; c < KS; ++c) kc[t][c] = buffer_load_u4(rk, n * (2 * D) + q * (D / 2) + c * 16);
+        for (int c = 0; c < KS; ++c) kc[t][c] = buffer_load_u4(rk, n * (2 * D) + 2 * k_dim(q, c));
     }
     __device__ __forceinline__ void issue_v(int t, __amdgpu_buffer_rsrc_t rv, int lane)
     {
@@ -380,9 +386,9 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
     static_assert(kCkTiles / kCkWaves <= 64, "block ids in one register");
     u32x4 q[D / 32];
     auto query = [&](const ChunkWork &w) {
-        const __half *rows = p.q + ((int64_t)w.b * p.n_q_heads + w.g * r + min(n, r - 1)) * D + quarter * (D / 4);
+        const __half *rows = p.q + ((int64_t)w.b * p.n_q_heads + w.g * r + min(n, r - 1)) * D;
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) q[s] = reinterpret_cast<const u32x4 *>(rows)[s];
+        for (int s = 0; s < D / 32; ++s) q[s] = *reinterpret_cast<const u32x4 *>(rows + Pair::k_dim(quarter, s));
     };
     // tiles past the wave's share: descriptors of no length (the loads take their turn and read nothing)
     auto tile = [&](const unsigned char *pool, const ChunkWork &w, int blocks, int pr, int h) {

@@ -583,53 +583,57 @@ __global__ void __launch_bounds__(kCkThreads) chunk_combine_kernel(ChunkParams p
     combine_heads<D, R, R>(lp, op, chunks, lse, 0, out, part);
 }
 
-// The weights of a chunk's tokens, and a share of the row's output rows; items as in chunk_kernel.
+// The weights of a row's tokens, and its output rows.  x: parts of a row, y: selected heads, z: sequences.  A
+// part takes every gridDim.x-th piece of the tokens, and of the first weight_parts(R) each a few heads' outputs.
+// (Numbered by the grid, not looked up like the items above: at a handful of loads a piece the look-up was half of
+// a workgroup's time; 384 rows of 2200 tokens, r = 8, 19.0 -> 12.4 us.)
+constexpr int weight_tokens(int R) { return kCkThreads * (R == 8 ? 2 : R == 4 ? 4 : 8); }        // of a piece
+constexpr int weight_parts(int R) { return R < 4 ? R : 4; }                                      // at least
 template <int D, int R>
 __global__ void __launch_bounds__(kCkThreads) chunk_weights_kernel(ChunkParams p)
 {
+    constexpr int HEADS = R / weight_parts(R);           // of a part
     __shared__ float lse[R];
     __shared__ f32x4 part[kCkThreads];
-    __shared__ int item[3];
-    __shared__ ChunkItems::Table table;
-    const int tid = threadIdx.x, wave = tid >> 6;
-    const ChunkItems items(p, table);
-    for (int64_t it = blockIdx.x; it < (int64_t)items.total * p.n_sel; it += gridDim.x) {
-        const int ci = (int)(it / p.n_sel), i = (int)(it % p.n_sel);
-        items.find(p, ci, item, table);
-        __syncthreads();
-        const int64_t b = item[0];
-        const int chunk = item[1], L = item[2];
-        const int chunks = chunks_of(L), t0 = chunk * kCkTokens, end = min(t0 + kCkTokens, L);
-        const int g = p.head_ids[i];
-        const int64_t row = b * p.n_sel + i;
-        const float *lp = p.lse_partial + row * p.max_chunks * R;
-        const float *sp = p.scores + row * R * p.slots;
-        const int64_t at = (b * p.n_kv_heads + g) * p.slots;
-        // a head that an earlier entry names is accumulated there
-        int named = 0;
-        for (int j = tid; j < i; j += kCkThreads) named |= p.head_ids[j] == g;
-        // scores and weights are on their way while the row's log-sum-exps are put together
-        constexpr int N = kCkTokens / kCkThreads;
-        float x[N][R], old[N];
+    const int tid = threadIdx.x, wave = tid >> 6, i = blockIdx.y;
+    const int64_t b = blockIdx.z, row = b * p.n_sel + i;
+    const int L = ChunkItems::length(p, (int)b), chunks = chunks_of(L);
+    const int pieces = (L + weight_tokens(R) - 1) / weight_tokens(R);
+    if ((int)blockIdx.x >= pieces && ((int)blockIdx.x >= weight_parts(R) || chunks == 1)) return;
+    const int g = p.head_ids[i];
+    const float *lp = p.lse_partial + row * p.max_chunks * R;
+    const float *sp = p.scores + row * R * p.slots;
+    const int64_t at = (b * p.n_kv_heads + g) * p.slots;
+    // scores and weights are on their way while the row's log-sum-exps are put together
+    constexpr int N = weight_tokens(R) / kCkThreads;
+    float x[N][R], old[N];
+    auto load = [&](int piece) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const int t = t0 + k * kCkThreads + tid;
+            const int t = (piece * N + k) * kCkThreads + tid;
             old[k] = 0.f;
-            if (t < end) {
+            if (t < L) {
 #pragma unroll
                 for (int j = 0; j < R; ++j) x[k][j] = sp[(int64_t)j * p.slots + t];
                 if (p.w_in && p.decay != 0.f) old[k] = p.w_in[at + t];
             }
         }
-        for (int j = wave; j < R; j += kCkWaves) {
-            const float v = row_lse(lp + j, R, chunks);
-            if ((tid & 63) == 0) lse[j] = v;
-        }
-        const bool again = __syncthreads_or(named);
+    };
+    load(blockIdx.x);
+    // a head that an earlier entry names is accumulated there
+    int named = 0;
+    for (int j = tid; j < i; j += kCkThreads) named |= p.head_ids[j] == g;
+    for (int j = wave; j < R; j += kCkWaves) {
+        const float v = row_lse(lp + j, R, chunks);
+        if ((tid & 63) == 0) lse[j] = v;
+    }
+    const bool again = __syncthreads_or(named);
+    for (int piece = blockIdx.x; piece < pieces && !again; piece += gridDim.x) {
+        if (piece != (int)blockIdx.x) load(piece);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const int t = t0 + k * kCkThreads + tid;
-            if (t < end && !again) {
+            const int t = (piece * N + k) * kCkThreads + tid;
+            if (t < L) {
                 float w = 0.f;
 #pragma unroll
                 for (int j = 0; j < R; ++j) w += fast_exp2(x[k][j] - lse[j]);
@@ -637,12 +641,11 @@ __global__ void __launch_bounds__(kCkThreads) chunk_weights_kernel(ChunkParams p
                 if (t == L - 1 && p.positions) p.positions[at + t] = p.n_seen[b] - 1;
             }
         }
-        if (chunks > 1)
-            for (int j = chunk; j < R; j += chunks)
-                combine_heads<D, R, 1>(lp, p.o_partial + row * p.max_chunks * R * D, chunks, lse, j,
-                                       p.out + (b * p.n_q_heads + g * R) * D, part);
-        __syncthreads();
     }
+    const int j0 = blockIdx.x * HEADS;
+    if (chunks > 1 && j0 < R)
+        combine_heads<D, R, HEADS>(lp, p.o_partial + row * p.max_chunks * R * D, chunks, lse, j0,
+                                   p.out + (b * p.n_q_heads + g * R) * D, part);
 }
 
 }  // namespace hetis

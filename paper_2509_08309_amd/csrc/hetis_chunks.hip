@@ -53,8 +53,10 @@ static int launch_chunks(const ChunkParams &p, int cus, hipStream_t st)
     auto finish = [&](auto group) {
         constexpr int R = decltype(group)::value;
         if constexpr (WEIGHTS) {
-            const unsigned wgs = (unsigned)std::min<int64_t>(most, (int64_t)cus * 8);
-            chunk_weights_kernel<D, R><<<wgs, kCkThreads, 0, st>>>(p);
+            // parts of a row: enough for eight workgroups a compute unit, where a row has that many pieces
+            const int64_t pieces = (p.slots + weight_tokens(R) - 1) / weight_tokens(R);
+            const int64_t parts = std::max<int64_t>(weight_parts(R), std::min<int64_t>(pieces, (int64_t)cus * 8 / ((int64_t)p.batch * p.n_sel)));
+            chunk_weights_kernel<D, R><<<dim3((unsigned)parts, p.n_sel, p.batch), kCkThreads, 0, st>>>(p);
         } else if (p.max_chunks > 1) {
             chunk_combine_kernel<D, R><<<dim3(p.n_sel, p.batch), kCkThreads, 0, st>>>(p);
         }

@@ -141,6 +141,22 @@ def test_weights_subset_workspace_and_graph_bit_for_bit(kv4):
         assert torch.equal(w, e) and np.array_equal(bits(o), out)
 
 
+@pytest.mark.parametrize("kv4", [False, True])
+@pytest.mark.parametrize("hq,hkv,heads", [(16, 2, [1]), (2, 2, [0, 1]), (8, 2, [0])])
+def test_weights_of_long_rows(kv4, hq, hkv, heads):
+    """More pieces than parts of a row, and a table far wider than the rows."""
+    a = Case(kv4, [9000, 0, 2050, 4095], hq, hkv, 64, seed=212, max_blocks=1200)
+    w_out = torch.full(a.w.shape, 3.0, device=DEV)
+    a.check(a.run(heads, 1.0, f32(a.w), w_out), heads, 1.0, w_out, np.full(a.w.shape, 3.0))
+
+
+def test_weights_of_many_short_rows():
+    lens = np.random.default_rng(213).integers(0, 70, 1100)
+    a = Case(True, lens, 2, 2, 64, seed=214)
+    w_out = torch.full(a.w.shape, 3.0, device=DEV)
+    a.check(a.run([0, 1], 0.5, f32(a.w), w_out), [0, 1], 0.5, w_out, np.full(a.w.shape, 3.0))
+
+
 # ------------------------------------------------------------------ the choice of slots
 
 class Rows:

@@ -134,6 +134,19 @@ def test_more_sequences_than_a_workgroup_has_threads():
     c.check(c.decode([1]), [1])
 
 
+def test_more_sequences_than_lengths_fit_on_chip():
+    lens = np.random.default_rng(18).integers(0, 20, 1500)
+    lens[[0, 1023, 1024, 1025, 1499]] = [530, 600, 1100, 513, 1030]
+    c = Cache4(lens, 2, 2, 64, seed=19)
+    c.check(c.decode([1]), [1])
+
+
+def test_more_heads_than_workgroups():
+    c = Cache4([20, 3, 520], 1024, 1024, 64, seed=28)
+    heads = list(np.random.default_rng(29).permutation(1024)[:1001])
+    c.check(c.decode(heads), heads)
+
+
 def test_scores_far_apart_and_equal():
     """One token that takes everything, thousands of equal ones, scores beyond what fp16 holds."""
     def dist(c):

@@ -16,7 +16,8 @@
  *     n_seen     int32 [B]           tokens that the sequence has seen so far, the newest included
  * Only rows of selected heads and slots in use are read or written.
  *
- * Conventions: those of hetis_attn.h.  Sequences that an eviction changes may not share blocks.
+ * Conventions: those of hetis_attn.h.  Sequences that an eviction changes may not share blocks.  batch <= 65535,
+ * n_kv_heads <= 1024, max_blocks_per_seq <= 2^24.
  */
 #ifndef HETIS_EVICT_H
 #define HETIS_EVICT_H

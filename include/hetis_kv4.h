@@ -29,7 +29,8 @@
  * skip entries that point outside the tables; the Attention calls do not check (hetis_attn_validate
  * does, for the same tables).
  *
- * Supported: head_dim in {64, 128}; block_size 16; Attention: r in {1, 2, 4, 8}.
+ * Supported: head_dim in {64, 128}; block_size 16; Attention: r in {1, 2, 4, 8}, batch <= 65535,
+ * n_kv_heads <= 1024, max_blocks_per_seq <= 2^24.  Pools, rows and queries start at 16-byte boundaries.
  */
 #ifndef HETIS_KV4_H
 #define HETIS_KV4_H
@@ -80,9 +81,10 @@ int hetis_kv4_fetch(const hetis_attn_shape *shape, const void *k_cache, const vo
  * through the workspace.
  *
  * hetis_attn_decode_kv4_ws: the caller's workspace, hetis_attn_decode_kv4_workspace_bytes(shape,
- *   n_sel_heads) bytes (it depends on batch, n_sel_heads, r, head_dim and max_blocks_per_seq).  It may
- *   be one that also serves the calls of hetis_attn.h (their control words and counters are left as
- *   they are), but not for launches that may run at the same time.
+ *   n_sel_heads) bytes (it depends on batch, n_sel_heads, r, head_dim and max_blocks_per_seq).  The rules
+ *   are those of hetis_attn_decode_ws: zeroed once before the first call (hetis_attn_workspace_init), every
+ *   launch leaves its counters at zero, one workspace for launches that may run at the same time.  One
+ *   workspace may serve these calls and those of hetis_attn.h.
  * hetis_attn_decode_kv4: on the library-owned workspace; the rules are those of hetis_attn_decode.
  * Errors: NULL, BAD_SHAPE, UNSUPPORTED, BAD_HEADS, WORKSPACE, ALLOC, LAUNCH.
  */

@@ -176,9 +176,11 @@ def test_head_subset_and_order_and_runs_bit_for_bit(D, r):
     assert np.array_equal(bits(c.decode([0, 1, 2, 3])), whole)
 
 
-def test_a_wider_block_table_changes_nothing():
-    a = Cache4([700, 40, 512], 8, 2, 128, seed=12)
-    b = Cache4([700, 40, 512], 8, 2, 128, seed=12, max_blocks=4000)
+@pytest.mark.parametrize("D,r", [(64, 1), (128, 1), (64, 2), (128, 2), (64, 4), (128, 4), (64, 8), (128, 8)])
+def test_a_wider_block_table_changes_nothing(D, r):
+    lens = [700, 40, 512, 4000, 1025, 9000, 2048]
+    a = Cache4(lens, 2 * r, 2, D, seed=12)
+    b = Cache4(lens, 2 * r, 2, D, seed=12, max_blocks=4000)
     b.table[:, :a.mb], b.k4, b.v4, b.q = a.table, a.k4, a.v4, a.q
     assert np.array_equal(bits(a.decode([0, 1])), bits(b.decode([0, 1])))
 
@@ -207,7 +209,9 @@ def test_workspaces_streams_and_graphs():
     want = bits(c.decode(heads))
     rc, n = H.hetis_attn_decode_kv4_workspace_bytes(c.shape(), 2)
     H.check(rc)
-    ws = [torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV) for _ in range(2)]      # contents mean nothing
+    ws = [torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    for w in ws:
+        H.check(H.hetis_attn_workspace_init(w, n))
     assert np.array_equal(bits(c.decode(heads, ws=ws[0])), want)
     # two graphs with a workspace each, replayed side by side and again, eager work in between
     q, k4, v4 = (torch.from_numpy(x).to(DEV) for x in (c.q, c.k4, c.v4))

@@ -257,6 +257,10 @@ __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const u
 struct ChunkItems {
     static constexpr int kMost = 1024;
     int total;                              // chunks of all sequences
+    // Up to 64 sequences: lane b of every wave has sequence b's first chunk number, the one after its last, its
+    // length, and an item is found by a ballot: no table, no barrier, which is up to a fifth of the smallest launches (8 to 30 short rows 6.4 -> 5.3 us).
+    bool few;
+    int start, end, len;
     __device__ static __forceinline__ int length(const ChunkParams &p, int b)
     {
         return min(max(p.seq_lens[b], 0), p.slots);
@@ -268,6 +272,21 @@ struct ChunkItems {
     __device__ __forceinline__ ChunkItems(const ChunkParams &p, Table &tab)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        few = p.batch <= 64;
+        if (few) {
+            len = lane < p.batch ? length(p, lane) : 0;
+            const int mine = lane < p.batch ? chunks_of(len) : 0;
+            end = mine;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(end, o);
+                end += lane >= o ? v : 0;
+            }
+            start = end - mine;
+            total = __builtin_amdgcn_readlane(end, 63);
+            return;
+        }
+        start = end = len = 0;
         const int span = (p.batch + kCkThreads - 1) / kCkThreads;
         int mine = 0;
         for (int b = tid * span; b < min((tid + 1) * span, p.batch); ++b) {
@@ -293,6 +312,16 @@ struct ChunkItems {
         tab.start[tid + 1] = upto;
         if (tid == 0) tab.start[0] = 0;
         __syncthreads();
+    }
+    // the same of `few`, by every wave (-1: past the last)
+    __device__ __forceinline__ int locate(int ci, int *chunk, int *L) const
+    {
+        const unsigned long long m = __ballot(ci >= start && ci < end);
+        if (m == 0) return -1;
+        const int b = __builtin_ctzll(m);
+        *chunk = ci - __builtin_amdgcn_readlane(start, b);
+        *L = __builtin_amdgcn_readlane(len, b);
+        return b;
     }
     // sequence, chunk and length of chunk number ci, by the thread that has it
     __device__ __forceinline__ void find(const ChunkParams &p, int ci, int *item, const Table &tab) const
@@ -323,20 +352,25 @@ struct ChunkLds {
 // Workgroups of a compute unit: as many as the registers of a lane allow.
 constexpr int chunk_residents(int D, bool kv4)
 {
-    return D == 64 ? 4 : kv4 ? 3 : 2;
+    return D == 64 ? (kv4 ? 4 : 3) : kv4 ? 3 : 2;
 }
 
 // A chunk of a sequence and a selected head, as a wave sees it (the same in all lanes).
 struct ChunkWork {
     int b, chunk, L, i, g;                  // b < 0: none
     int tokens, last_tile, p0, np;          // of the chunk; its last tile in the row; the wave's pairs
-    __device__ __forceinline__ void set(const ChunkParams &p, const int *item, int head, int wave)
+    // item `ci`, looked up in `item` or found here; `head_id`: of the selected head `head`
+    __device__ __forceinline__ void set(const ChunkItems &items, int ci, const int *item, int head, int head_id, int wave)
     {
-        b = __builtin_amdgcn_readfirstlane(item[0]);
-        chunk = __builtin_amdgcn_readfirstlane(item[1]);
-        L = __builtin_amdgcn_readfirstlane(item[2]);
+        if (items.few) {
+            b = items.locate(ci, &chunk, &L);
+        } else {
+            b = __builtin_amdgcn_readfirstlane(item[0]);
+            chunk = __builtin_amdgcn_readfirstlane(item[1]);
+            L = __builtin_amdgcn_readfirstlane(item[2]);
+        }
         i = head;
-        g = b < 0 ? 0 : head_id(p, head);
+        g = head_id;
         tokens = min(L - chunk * kCkTokens, kCkTokens);
         const int tiles = (tokens + kBlockTokens - 1) / kBlockTokens;
         last_tile = chunk * kCkTiles + tiles - 1;
@@ -357,7 +391,6 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, quarter = lane >> 4, r = p.group;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     constexpr int kFoldDims = kCkMaxGroup * D / kCkThreads;
-    const ChunkItems items(p, lds.table);
     // (chunk number, selected head) of an item, and of the workgroup's next one
     struct At {
         int chunk, head;
@@ -372,7 +405,12 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
         }
         return a;
     };
+    // the first two items' heads are on their way while the lengths are
+    At at{(int)(blockIdx.x / p.n_sel), (int)(blockIdx.x % p.n_sel)};
+    const int first_head = head_id(p, at.head), second_head = head_id(p, after(at).head);
+    const ChunkItems items(p, lds.table);
     auto look_up = [&](At a, int turn) {
+        if (items.few) return;
         if (a.chunk < items.total)
             items.find(p, a.chunk, lds.item[turn], lds.table);
         else if (tid == 0)
@@ -405,17 +443,18 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
         for (int h = 0; h < 2; ++h) t.issue_v(h, tile(p.v, w, blocks, pr, h), lane);
     };
 
-    At at{(int)(blockIdx.x / p.n_sel), (int)(blockIdx.x % p.n_sel)};
     if (at.chunk >= items.total) return;
     ChunkWork cur, nxt;
-    look_up(at, 0);
-    look_up(after(at), 1);
-    __syncthreads();
-    cur.set(p, lds.item[0], at.head, wave);
+    if (!items.few) {
+        look_up(at, 0);
+        look_up(after(at), 1);
+        __syncthreads();
+    }
+    cur.set(items, at.chunk, lds.item[0], at.head, first_head, wave);
     at = after(at);
-    nxt.set(p, lds.item[1], at.head, wave);
+    nxt.set(items, at.chunk, lds.item[1], at.head, second_head, wave);
     at = after(at);                                      // the item after next
-    __syncthreads();
+    if (!items.few) __syncthreads();
     int blocks = 0, next_blocks = 0;
     Pair x;
     if (cur.np > 0) {
@@ -506,7 +545,7 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
         if (nxt.b < 0) return;
         cur = nxt;
         blocks = next_blocks;
-        nxt.set(p, lds.item[turn], at.head, wave);
+        nxt.set(items, at.chunk, lds.item[turn], at.head, head_id(p, at.head), wave);
         at = after(at);
     }
 }

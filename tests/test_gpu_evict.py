@@ -150,6 +150,20 @@ def test_weights_of_long_rows(kv4, hq, hkv, heads):
     a.check(a.run(heads, 1.0, f32(a.w), w_out), heads, 1.0, w_out, np.full(a.w.shape, 3.0))
 
 
+@pytest.mark.parametrize("kv4", [False, True])
+def test_weights_of_many_items_and_few_bit_for_bit(kv4):
+    lens = np.random.default_rng(215).integers(1, 2300, 130)
+    lens[:10] = [0, 512, 513, 1024, 1025, 1536, 1537, 2048, 2049, 4097]
+    a = Case(kv4, lens, 32, 8, 64, seed=216)
+    whole, w_in = torch.zeros(a.w.shape, device=DEV), f32(a.w)
+    out = bits(a.run(list(range(8)), 0.5, w_in, whole))
+    for heads in ([5], [2, 0]):
+        w = torch.zeros(a.w.shape, device=DEV)
+        rows = [g * 4 + j for g in heads for j in range(4)]
+        assert np.array_equal(bits(a.run(heads, 0.5, w_in, w))[:, rows], out[:, rows])
+        assert torch.equal(w[:, heads], whole[:, heads])
+
+
 def test_weights_of_many_short_rows():
     lens = np.random.default_rng(213).integers(0, 70, 1100)
     a = Case(True, lens, 2, 2, 64, seed=214)

@@ -185,6 +185,29 @@ def test_a_wider_block_table_changes_nothing(D, r):
     assert np.array_equal(bits(a.decode([0, 1])), bits(b.decode([0, 1])))
 
 
+@pytest.mark.parametrize("D,r", [(64, 4), (128, 8), (64, 2)])
+def test_many_items_and_few_bit_for_bit(D, r):
+    """A call of more items than workgroups against calls of fewer: the same bits."""
+    rng = np.random.default_rng(30)
+    lens = rng.integers(1, 2300, 130)
+    lens[:12] = [0, 512, 513, 1024, 1025, 1536, 1537, 2048, 2049, 511, 1023, 4097]
+    c = Cache4(lens, 8 * r, 8, D, seed=31)
+    k4, v4 = torch.from_numpy(c.k4).to(DEV), torch.from_numpy(c.v4).to(DEV)
+    out = c.decode(list(range(8)), k4=k4, v4=v4)
+    whole = bits(out)
+    for heads in ([5], [2, 0]):
+        got = bits(c.decode(heads, k4=k4, v4=v4))
+        rows = [g * r + j for g in heads for j in range(r)]
+        assert np.array_equal(got[:, rows], whole[:, rows])
+    few = np.array([b for b in range(130) if b < 12 or b % 10 == 0])
+    for b in few:
+        for g in (0, 7):
+            if c.lens[b]:
+                k, v = c.rows(b, g)
+                ref, _, tol = attention_bound(c.q[b, g * r:(g + 1) * r].astype(np.float64), k, v, c.scale)
+                assert (np.abs(out[b, g * r:(g + 1) * r].cpu().numpy() - ref) <= tol).all(), (b, g)
+
+
 def test_strides_and_offsets_past_32_bits():
     """Head-major pools, and blocks 100 MB apart in a pool of 8 GB."""
     c = Cache4([300, 20, 600], 4, 2, 128, seed=13)

@@ -7,8 +7,8 @@
  *
  * Values.  A row of D fp16 values is cut into groups of HETIS_KV4_GROUP = 32.  With lo and hi the
  * smallest and largest value of a group (fp32 arithmetic, f16() rounds to nearest even)
- *     s = f16((hi - lo) / 15)     b = f16(lo - 16 s)     c = clamp(rint((x - b) / s - 16), 0, 15)
- * (c = 0 where s = 0) and the value held is f16(s * (16 + c) + b), rounded once.  Values are first
+ *     s = f16((hi - lo) * f32(1 / 15))     b = f16(lo - 16 s)     c = clamp(rint((x - b) / s - 16), 0, 15)
+ * (a product with the fp32 number nearest to 1 / 15; c = 0 where s = 0) and the value held is f16(s * (16 + c) + b), rounded once.  Values are first
  * cut to +-20480, so that b is finite; a group with a NaN holds NaN throughout (s = b = NaN, c = 0).  Attention and
  * hetis_kv4_fetch use exactly the values held.
  *

@@ -62,7 +62,15 @@ __device__ __forceinline__ float quad_swap2(float x)
     return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xf, 0xf, true));
 }
 
-// The quotients are those of an IEEE division: a code lies next to a border wherever the values of a group lie
+// An fp32 number as fp16.  (The compiler would make one v_fma_mixlo_f16 of a product and its conversion, which
+// leaves out the rounding to fp32 that the definition has: another s wherever the product lies between two.)
+__device__ __forceinline__ __half kv4_half_of(float x)
+{
+    asm("" : "+v"(x));
+    return __float2half_rn(x);
+}
+
+// The quotients (x - b) / s are those of an IEEE division: a code lies next to a border wherever the values of a group lie
 // on a grid, and a reciprocal alone would move such values to the other side.  A product with the reciprocal
 // (rounded, and of a rounded reciprocal: off by at most 3 * 2^-24 * 31 < 6e-6, the division by 2e-6) says how near
 // to a border a value is; only where one of a thread's eight is within 2e-5 are they divided (a store of
@@ -87,9 +95,9 @@ __device__ __forceinline__ Kv4Piece kv4_quantise(const kv_u32x4 raw)
     lo = fminf(lo, quad_swap2(lo));
     hi = fmaxf(hi, quad_swap2(hi));
     Kv4Piece r;
-    r.s = __float2half_rn((hi - lo) / 15.f);
+    r.s = kv4_half_of((hi - lo) * (1.f / 15.f));
     float s = __half2float(r.s);
-    r.b = __float2half_rn(lo - 16.f * s);
+    r.b = kv4_half_of(lo - 16.f * s);
     if (nan) {
         r.s = r.b = __ushort_as_half(0x7e00);
         s = 0.f;

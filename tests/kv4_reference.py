@@ -11,7 +11,7 @@ def quantise(x):
     bad = np.isnan(g).any(-1)
     g = np.clip(np.nan_to_num(g, nan=0.0, posinf=LIMIT, neginf=-LIMIT), -LIMIT, LIMIT)
     lo, hi = g.min(-1), g.max(-1)
-    s = ((hi - lo).astype(np.float32) / np.float32(15)).astype(np.float16).astype(np.float64)
+    s = ((hi - lo).astype(np.float32) * (np.float32(1) / np.float32(15))).astype(np.float16).astype(np.float64)
     b = (lo - 16 * s).astype(np.float32).astype(np.float16).astype(np.float64)
     with np.errstate(divide="ignore", invalid="ignore"):
         # the quotient in fp32, as the definition has it

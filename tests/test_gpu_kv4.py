@@ -319,6 +319,27 @@ def test_store_and_fetch(D, seed):
         assert (got[:, [0, 2]] == 7.0).all()
 
 
+def test_scales_half_way_between_two_numbers():
+    """(hi - lo) / 15 = 1 + (2 k + 1) / 2048: which fp16 number is taken depends on the rounding of the fp32 product."""
+    c = Cache4([68], 1, 1, 64, seed=23)
+    kn = np.zeros((68, 1, 64), dtype=np.float16)
+    for k in range(68):
+        hi = np.float16(15 * (2 * k + 1) / 2048)
+        assert float(hi) + 15 == 15 * (1 + (2 * k + 1) / 2048)
+        kn[k, 0, 0::32], kn[k, 0, 1::32] = -15, hi
+    vn = (kn * np.float16(0.25)).astype(np.float16)
+    seq, pos = np.zeros(68, dtype=np.int32), np.arange(68, dtype=np.int32)
+    k4, v4 = torch.from_numpy(c.k4).to(DEV), torch.from_numpy(c.v4).to(DEV)
+    H.check(H.hetis_kv4_store(c.shape(), torch.from_numpy(kn).to(DEV), torch.from_numpy(vn).to(DEV), i32(seq), i32(pos),
+                              68, i32(c.table), i32([0]), 1, c.nb, k4, v4))
+    want_k, want_v = c.k4.copy(), c.v4.copy()
+    for t in range(68):
+        R.put_row(want_k[c.table[0, t // 16], 0], c.places[0], t % 16, kn[t, 0])
+        R.put_row(want_v[c.table[0, t // 16], 0], c.places[1], t % 16, vn[t, 0])
+    assert_same(k4, want_k)
+    assert_same(v4, want_v)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_append(D):
     c = Cache4([1, 15, 16, 17, 0, 33, 160], 4, 4, D, seed=22)

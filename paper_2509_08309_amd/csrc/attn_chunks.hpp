@@ -7,7 +7,11 @@
 //                      (A) and of query head n (B); which ones is the cache's choice (k_dim), the same for both.
 //   O^T += V^T . P     v_mfma_f32_16x16x32_f16 over 32 tokens: lane l holds, of tokens 4 q .. 4 q + 3 of both
 //                      tiles, dim n D/16 + j (A, row block j) and the probabilities of head n (B), which are
-//                      what the first product and exp2 leave in its registers.
+//                      what the first product and exp2 leave in its registers.  A group has at most 8 heads:
+//                      columns n and n + 8 are the same head, the first with the probability cut to fp16, the
+//                      second with what the cut left over, so that the sums hold 21 bits of a probability
+//                      (rounded to fp16 alone, outputs were off by 2.8e-4 of them, now by 1.8e-4, which is their
+//                      own rounding; 32 long rows of 13 heads 61.3 -> 62.4 us, calls in a row).
 //
 // A row (sequence, head) is cut into chunks of kCkTokens tokens, always at the same places; the four waves
 // of a workgroup take a quarter of a chunk's tile pairs each and fold their sums through LDS.  Rows of more
@@ -195,6 +199,12 @@ struct ChunkState {
     f32x4 acc[D / 16];
 };
 
+// The value of the lane 8 further on in the row of 16.
+__device__ __forceinline__ float row_rotate8(float x)
+{
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xf, 0xf, true));
+}
+
 // Two tiles; RAGGED: of their 32 tokens the first `left` count.
 // `next_k` asks for the K part of the next two once this one's has been used.
 template <int D, class Pair, bool SCORES, bool RAGGED, class Next>
@@ -234,21 +244,29 @@ __device__ __forceinline__ void chunk_update(ChunkState<D> &st, Pair &t, const u
         for (int j = 0; j < D / 16; ++j) st.acc[j] *= alpha;
     }
     const float down = -st.m * scale_log2;
-    f16x8 p;
+    const float cut = lane & 8 ? -1.f : 0.f;
+    u32x4 p;
     float ps = 0.f;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float x = fast_exp2(__builtin_fmaf(c[i][e], scale_log2, down));
-            if (RAGGED && i * 16 + (lane >> 4) * 4 + e >= left) x = 0.f;     // (a scale of 0: inf * 0)
-            ps += x;
-            p[4 * i + e] = (_Float16)x;                 // (fp16 products; the sum is of what was not rounded)
+        for (int e = 0; e < 4; e += 2) {
+            float x[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                x[k] = fast_exp2(__builtin_fmaf(c[i][e + k], scale_log2, down));
+                if (RAGGED && i * 16 + (lane >> 4) * 4 + e + k >= left) x[k] = 0.f;  // (a scale of 0: inf * 0)
+                ps += x[k];
+            }
+            // towards zero: what is left over is not negative, and an infinite value stays itself
+            const f16x2 hi = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(x[0], x[1]));
+            p[2 * i + e / 2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(
+                __builtin_fmaf((float)hi[0], cut, x[0]), __builtin_fmaf((float)hi[1], cut, x[1])));
         }
     st.l += ps;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j)
-        st.acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.v(j), p, st.acc[j], 0, 0, 0);
+        st.acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(t.v(j), __builtin_bit_cast(f16x8, p), st.acc[j], 0, 0, 0);
 }
 
 // Items are (chunk of a sequence, selected head), heads fastest; workgroups stride over them.  Thread t looks
@@ -424,7 +442,7 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
     static_assert(kCkTiles / kCkWaves <= 64, "block ids in one register");
     u32x4 q[D / 32];
     auto query = [&](const ChunkWork &w) {
-        const __half *rows = p.q + ((int64_t)w.b * p.n_q_heads + w.g * r + min(n, r - 1)) * D;
+        const __half *rows = p.q + ((int64_t)w.b * p.n_q_heads + w.g * r + min(n & 7, r - 1)) * D;
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) q[s] = *reinterpret_cast<const u32x4 *>(rows + Pair::k_dim(quarter, s));
     };
@@ -475,7 +493,7 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
         const int64_t row = (int64_t)cur.b * p.n_sel + cur.i;
         if (cur.np > 0) {
             // columns without a head are zero
-            const unsigned has = n < r ? ~0u : 0u;
+            const unsigned has = (n & 7) < r ? ~0u : 0u;
 #pragma unroll
             for (int s = 0; s < D / 32; ++s) q[s] = (q[s] ^ p.q_sign) & has;
             float *scores = nullptr;
@@ -498,6 +516,16 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
             issue_v(x, nxt, next_blocks, 0);
         }
         st.l = sum_xor32(sum_xor16(st.l));
+        // The two columns of a head.  (Of an fp16 cache's infinite values an infinite sum is one by its first
+        // column; 0 * inf may be in the second.  4-bit values are finite or NaN.)
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float more = row_rotate8(st.acc[j][e]);
+                const bool alone = !KV4 && fabsf(st.acc[j][e]) == INFINITY;
+                st.acc[j][e] = alone ? st.acc[j][e] : st.acc[j][e] + more;
+            }
         if (n < r) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -587,7 +615,8 @@ __device__ __forceinline__ void combine_heads(const float *lp, const float *op, 
             v[e] = *reinterpret_cast<const f32x4 *>(op + (int64_t)ce * R * D + at);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o += v[e] * (c + e * G < chunks ? fast_exp2(w[e] - all) : 0.f);
+        for (int e = 0; e < 8; ++e)
+            if (c + e * G < chunks) o += v[e] * fast_exp2(w[e] - all);      // (no 0 * inf of a chunk read twice)
     }
     if constexpr (G > 1) {
         __syncthreads();

@@ -164,6 +164,24 @@ def test_weights_of_many_items_and_few_bit_for_bit(kv4):
         assert torch.equal(w[:, heads], whole[:, heads])
 
 
+@pytest.mark.parametrize("D,hq,hkv", [(64, 4, 4), (128, 16, 2)])
+def test_infinite_values(D, hq, hkv):
+    """Equal probabilities: an infinite value of the fp16 cache is what its dim comes to, and no other dim's matter."""
+    a = Case(False, [1, 40, 700], hq, hkv, D, seed=215)
+    c = a.c
+    c.q[:] = 0
+    for b, L in enumerate(c.lens):
+        for g in range(hkv):
+            for t, d, x in ((0, 3, np.inf), (L - 1, 9, -np.inf), (L // 2, D - 1, np.inf)):
+                c.v[c.table[b, t // 16], g, t % 16, d] = x
+    a.v = torch.from_numpy(c.v).to(DEV)
+    w = torch.full(a.w.shape, 3.0, device=DEV)
+    out = a.run(list(range(hkv)), 0.0, None, w).cpu().numpy()
+    assert (out[..., [3, D - 1]] == np.inf).all() and (out[..., 9] == -np.inf).all()
+    others = [d for d in range(D) if d not in (3, 9, D - 1)]
+    assert np.isfinite(out[..., others]).all()
+
+
 def test_weights_of_many_short_rows():
     lens = np.random.default_rng(213).integers(0, 70, 1100)
     a = Case(True, lens, 2, 2, 64, seed=214)

@@ -96,15 +96,15 @@ class Cache4:
 
 
 def attention_bound(q, k, v, scale):
-    """Reference and how far an output may be from it.  A probability is rounded to fp16 (2^-11 of it, or 2^-25 of the
-    largest where it is subnormal: 2^-25 sum |v|, the largest being exp2(0) = 1 and the sum of all at least 1), an
-    output once more; a score is a sum of D products in fp32 (each partial sum at most S = the largest sum of |q k|,
+    """Reference and how far an output may be from it.  A probability is held in two fp16 numbers, both cut towards
+    zero (2^-20 of it, or 2^-24 of the largest where the second is subnormal: 2^-24 sum |v|, the largest being
+    exp2(0) = 1 and the sum of all at least 1), an output is rounded to fp16; a score is a sum of D products in fp32 (each partial sum at most S = the largest sum of |q k|,
     (D + 4) 2^-24 S), scaled and subtracted from the running maximum (3 roundings of at most |s|), and the error of
     a score is the relative error of its probability, twice because of the sum; 2^-20 for the exponentials, the sums
     over waves and chunks and the divisions."""
     ref, p, pv, sv, s_max, S = R.attend(q, k, v, scale)
     delta = 2 * ((q.shape[1] + 4) * 2.0 ** -24 * S + 3 * 2.0 ** -23 * s_max) + 2.0 ** -20
-    return ref, p, (2.0 ** -11 + delta) * pv + 2.0 ** -25 * sv[None] + 2.0 ** -11 * np.abs(ref) + 2.0 ** -24
+    return ref, p, (2.0 ** -20 + delta) * pv + 2.0 ** -24 * sv[None] + 2.0 ** -11 * np.abs(ref) + 2.0 ** -24
 
 
 EDGES = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 159, 255, 256, 257, 384, 511, 512, 513, 640, 1023, 1024,

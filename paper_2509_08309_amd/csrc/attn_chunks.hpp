@@ -276,7 +276,8 @@ struct ChunkItems {
     static constexpr int kMost = 1024;
     int total;                              // chunks of all sequences
     // Up to 64 sequences: lane b of every wave has sequence b's first chunk number, the one after its last, its
-    // length, and an item is found by a ballot: no table, no barrier, which is up to a fifth of the smallest launches (8 to 30 short rows 6.4 -> 5.3 us).
+    // length, and an item is found by a ballot: no table, no barrier, which is up to a fifth of the smallest
+    // launches (8 to 30 short rows 6.4 -> 5.3 us).
     bool few;
     int start, end, len;
     __device__ static __forceinline__ int length(const ChunkParams &p, int b)

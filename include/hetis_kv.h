@@ -138,7 +138,7 @@ int hetis_kv_copy_tiles(const hetis_kv_pool *src_pool, const void *src_k, const 
 
 /*
  * Measurement hook, like hetis_attn_profile_events: the two events are attached to
- * the kernel dispatch of every later hetis_kv_* call of the same host thread
+ * the kernel dispatch of every later hetis_kv_* and hetis_kv4_* call of the same host thread
  * (start when the kernel begins to execute, stop when it has finished).
  * (NULL, NULL) switches it off.
  */

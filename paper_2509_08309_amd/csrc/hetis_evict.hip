@@ -6,6 +6,7 @@
 
 #include "cache_checks.hpp"
 #include "evict.hpp"
+#include "kv_launch.hpp"
 
 namespace hetis {
 
@@ -39,14 +40,11 @@ static int move_call(bool kv4, const hetis_attn_shape *shape, const int32_t *mov
     const dim3 grid((unsigned)std::min<int64_t>(((int64_t)max_moves + per_wg - 1) / per_wg, (int64_t)1 << 23),
                     (unsigned)n_sel, (unsigned)shape->batch);
     const hipStream_t st = (hipStream_t)stream;
-    if (shape->head_dim == 128) {
-        if (kv4) kv_move_rows_kernel<128, true><<<grid, kKvRowThreads, 0, st>>>(p);
-        else kv_move_rows_kernel<128, false><<<grid, kKvRowThreads, 0, st>>>(p);
-    } else {
-        if (kv4) kv_move_rows_kernel<64, true><<<grid, kKvRowThreads, 0, st>>>(p);
-        else kv_move_rows_kernel<64, false><<<grid, kKvRowThreads, 0, st>>>(p);
-    }
-    return launched();
+    if (shape->head_dim == 128)
+        return kv4 ? launch_kv(kv_move_rows_kernel<128, true>, grid, st, p, true, true, kKvRowThreads)
+                   : launch_kv(kv_move_rows_kernel<128, false>, grid, st, p, true, true, kKvRowThreads);
+    return kv4 ? launch_kv(kv_move_rows_kernel<64, true>, grid, st, p, true, true, kKvRowThreads)
+               : launch_kv(kv_move_rows_kernel<64, false>, grid, st, p, true, true, kKvRowThreads);
 }
 
 }  // namespace hetis
@@ -96,11 +94,10 @@ int hetis_kv_evict(const hetis_attn_shape *shape, const float *weights_in, const
     // threads 14.2 us, 256 with 16 keys 16.0), one window as far as registers go (64 rows of 8k to 24k: 32
     // keys 36.9 us, two windows of 16 keys 52.7; 208 rows of 2k to 12k: 1024 threads 23.6, 512 with 32 keys
     // 30.1).
-    if (p.slots <= 512 * 8) evict_kernel<512, 8, true><<<grid, 512, 0, st>>>(p);
-    else if (p.slots <= 1024 * 16) evict_kernel<1024, 16, true><<<grid, 1024, 0, st>>>(p);
-    else if (p.slots <= 1024 * 32) evict_kernel<1024, 32, true><<<grid, 1024, 0, st>>>(p);
-    else evict_kernel<1024, 16, false><<<grid, 1024, 0, st>>>(p);
-    return launched();
+    if (p.slots <= 512 * 8) return launch_kv(evict_kernel<512, 8, true>, grid, st, p, true, true, 512);
+    if (p.slots <= 1024 * 16) return launch_kv(evict_kernel<1024, 16, true>, grid, st, p, true, true, 1024);
+    if (p.slots <= 1024 * 32) return launch_kv(evict_kernel<1024, 32, true>, grid, st, p, true, true, 1024);
+    return launch_kv(evict_kernel<1024, 16, false>, grid, st, p, true, true, 1024);
 }
 
 int hetis_kv_move(const hetis_attn_shape *shape, const int32_t *move_src, const int32_t *move_dst,

@@ -2,11 +2,10 @@
 // Argument errors are reported before the first HIP call.
 #include "../../include/hetis_kv.h"
 
-#include <hip/hip_ext.h>
-
 #include <algorithm>
 
 #include "kv_cache.hpp"
+#include "kv_launch.hpp"
 
 namespace hetis {
 
@@ -53,23 +52,8 @@ static int check_pool(const hetis_kv_pool *pl, KvChecked *c)
 constexpr int64_t kMaxGridX = (int64_t)1 << 23;
 constexpr int64_t kMaxGridY = 65535;
 
-// Optional events attached to the kernel's dispatch (measurement hook, per host thread):
-// start is stamped when the kernel begins to execute, stop when it has finished.
-static thread_local hipEvent_t t_kv_begin = nullptr;
-static thread_local hipEvent_t t_kv_end = nullptr;
-
-// `first` / `last`: of the launches of one call.
-template <class Kernel, class Params>
-static int launch_kv(Kernel kernel, dim3 grid, hipStream_t st, const Params &p, bool first = true,
-                     bool last = true)
-{
-    if (t_kv_begin)
-        hipExtLaunchKernelGGL(kernel, grid, dim3(256), 0, st, first ? t_kv_begin : nullptr,
-                              last ? t_kv_end : nullptr, 0, p);
-    else
-        kernel<<<grid, 256, 0, st>>>(p);
-    return hipGetLastError() == hipSuccess ? HETIS_OK : HETIS_ERR_LAUNCH;
-}
+thread_local hipEvent_t t_kv_begin = nullptr;
+thread_local hipEvent_t t_kv_end = nullptr;
 
 // One workgroup per (selected head, group of entries), within the limits of a grid.
 static int launch_rows(bool fetch, const hetis_attn_shape *s, const KvChecked &c, KvRowParams p,

@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "cache_checks.hpp"
+#include "kv_launch.hpp"
 
 namespace hetis {
 
@@ -48,14 +49,9 @@ static int kv4_rows_call(bool fetch, const hetis_attn_shape *shape, const void *
     const dim3 grid((unsigned)std::min<int64_t>(n_sel, kMaxGridX),
                     (unsigned)std::min<int64_t>((n_tokens + per_wg - 1) / per_wg, kMaxGridY));
     const hipStream_t st = (hipStream_t)stream;
-    if (D == 128) {
-        if (fetch) kv4_rows_kernel<128, true><<<grid, kKvRowThreads, 0, st>>>(p);
-        else kv4_rows_kernel<128, false><<<grid, kKvRowThreads, 0, st>>>(p);
-    } else {
-        if (fetch) kv4_rows_kernel<64, true><<<grid, kKvRowThreads, 0, st>>>(p);
-        else kv4_rows_kernel<64, false><<<grid, kKvRowThreads, 0, st>>>(p);
-    }
-    return launched();
+    if (D == 128)
+        return fetch ? launch_kv(kv4_rows_kernel<128, true>, grid, st, p) : launch_kv(kv4_rows_kernel<128, false>, grid, st, p);
+    return fetch ? launch_kv(kv4_rows_kernel<64, true>, grid, st, p) : launch_kv(kv4_rows_kernel<64, false>, grid, st, p);
 }
 
 }  // namespace hetis

@@ -410,3 +410,31 @@ def test_evicted_cache_in_the_other_calls():
             k, v = a.rows(b, g)
             ref = R.attend(c.q[b, g * 4:g * 4 + 4].astype(np.float64), k[keep], v[keep], c.scale)[0]
             assert np.abs(got[b, g * 4:g * 4 + 4] - ref).max() <= 4e-3
+
+
+@pytest.mark.parametrize("kv4", [False, True])
+def test_profile_events_carry_the_calls(kv4):
+    """hetis_kv_profile_events: stamped anew by a choice of slots, by moves and by rows stored in 4 bits."""
+    a = Rows([700, 40], 4, 41, "spread")
+    c = Cache4([700, 40], 4, 4, 64, seed=42)
+    k, v = (torch.from_numpy(x).to(DEV) for x in ((c.k4, c.v4) if kv4 else (c.k, c.v)))
+    src, dst = (torch.full((2, 1, 4), -1, dtype=torch.int32, device=DEV) for _ in range(2))
+    move = H.hetis_kv4_move if kv4 else H.hetis_kv_move
+    rows = torch.zeros(2, 4, 64, dtype=torch.float16, device=DEV)
+    calls = [lambda: H.check(move(c.shape(), src, dst, 4, i32(c.table), i32([1]), 1, c.nb, k, v)), lambda: a.run([1], [64, 64], 4, 8, 100)]
+    if kv4:
+        calls.append(lambda: H.check(H.hetis_kv4_append(c.shape(), rows, rows, i32(c.table), i32(c.lens), i32([1]), 1, c.nb, k, v)))
+    for call in calls:
+        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        begin.record()
+        torch.zeros(1 << 28, dtype=torch.uint8, device=DEV)
+        end.record()
+        torch.cuda.synchronize()
+        old = begin.elapsed_time(end)
+        assert H.hetis_kv_profile_events(begin.cuda_event, end.cuda_event) == 0
+        try:
+            call()
+        finally:
+            H.hetis_kv_profile_events(None, None)
+        torch.cuda.synchronize()
+        assert 0.0 < begin.elapsed_time(end) < 5.0 and begin.elapsed_time(end) != old

@@ -27,7 +27,7 @@
  * unless marked host, calls enqueue on `stream` and return a status, argument errors are detected
  * before the first HIP call; the row calls check every index that they read from device memory and
  * skip entries that point outside the tables; the Attention calls do not check (hetis_attn_validate
- * does, for the same tables).
+ * does, for the same tables; its strides are an fp16 cache's, so it is given a shape with strides of 0).
  *
  * Supported: head_dim in {64, 128}; block_size 16; Attention: r in {1, 2, 4, 8}, batch <= 65535,
  * n_kv_heads <= 1024, max_blocks_per_seq <= 2^24.  Pools, rows and queries start at 16-byte boundaries.

@@ -336,7 +336,10 @@ struct ChunkItems {
     __device__ __forceinline__ int locate(int ci, int *chunk, int *L) const
     {
         const unsigned long long m = __ballot(ci >= start && ci < end);
-        if (m == 0) return -1;
+        if (m == 0) {
+            *chunk = *L = 0;
+            return -1;
+        }
         const int b = __builtin_ctzll(m);
         *chunk = ci - __builtin_amdgcn_readlane(start, b);
         *L = __builtin_amdgcn_readlane(len, b);

@@ -402,6 +402,37 @@ struct ChunkWork {
     }
 };
 
+// The sums (largest score M) of those of a thread's dims from d that have become NaN, once more token by token, where an
+// infinite value is what its dim comes to however small its token's probability is.  (In the products above the
+// probability may be 0 in both fp16 numbers, and 0 * inf is NaN.)  `sp`: the row's scores, which the workgroup's waves
+// have stored.  Hardly ever taken, and the test for it does not show (weights beside Attention of 32 x 32 heads 108.8
+// us without it, 108.8 with it).
+template <int D, int N>
+__device__ __forceinline__ void infinite_dims(const ChunkParams &p, const ChunkWork &w, const float *sp, int d, float M,
+                                              float (&o)[N])
+{
+    bool lost = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) lost |= o[e] != o[e];
+    if (!lost) return;
+    float s[N] = {};
+#pragma unroll 1
+    for (int t = 0; t < w.tokens; ++t) {
+        const int slot = w.chunk * kCkTokens + t;
+        const int64_t block = p.block_table[(int64_t)w.b * p.max_blocks_per_seq + slot / kBlockTokens];
+        const __half *v = reinterpret_cast<const __half *>(p.v + block * p.stride_block + (int64_t)w.g * p.stride_head) +
+                          slot % kBlockTokens * D + d;
+        const float x = sp[slot], pr = fast_exp2(x - M);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float f = __half2float(v[e]);
+            s[e] += fabsf(f) == INFINITY && x > -INFINITY ? f : pr * f;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) o[e] = o[e] != o[e] ? s[e] : o[e];
+}
+
 // One barrier an item: the first tiles, the query rows and the block ids of the next item are asked for before
 // the waves' results of this one are folded, the item after next is looked up meanwhile, and what the waves
 // leave in LDS alternates between two places.
@@ -521,7 +552,8 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
         }
         st.l = sum_xor32(sum_xor16(st.l));
         // The two columns of a head.  (Of an fp16 cache's infinite values an infinite sum is one by its first
-        // column; 0 * inf may be in the second.  4-bit values are finite or NaN.)
+        // column; 0 * inf may be in the second.  Where it is in the first, see infinite_dims.  4-bit values are
+        // finite or NaN.)
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
 #pragma unroll
@@ -559,6 +591,7 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
             for (int w = 0; w < kCkWaves; ++w)
 #pragma unroll
                 for (int e = 0; e < kFoldDims; ++e) o[e] += f[w] * lds.o[turn][w][j][d + e];
+            if constexpr (!KV4) infinite_dims<D>(p, cur, p.scores + (row * r + j) * p.slots, d, M, o);
             const float inv = cur.tokens > 0 ? 1.f / sum : 0.f;
 #pragma unroll
             for (int e = 0; e < kFoldDims; ++e) o[e] = cur.tokens > 0 ? o[e] * inv : 0.f;
@@ -622,6 +655,19 @@ __device__ __forceinline__ void combine_heads(const float *lp, const float *op, 
         for (int e = 0; e < 8; ++e)
             if (c + e * G < chunks) o += v[e] * fast_exp2(w[e] - all);      // (no 0 * inf of a chunk read twice)
     }
+    // (as in infinite_dims: chunks whose weight is 0 in fp32)
+    if (o[0] + o[1] + o[2] + o[3] != o[0] + o[1] + o[2] + o[3]) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int c = grp; c < chunks; c += G) {
+            const float w = lp[c * R + j], f = fast_exp2(w - all);
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(op + (int64_t)c * R * D + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += fabsf(v[e]) == INFINITY && w > -INFINITY ? v[e] : v[e] * f;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = o[e] != o[e] ? s[e] : o[e];
+    }
     if constexpr (G > 1) {
         __syncthreads();
         part[threadIdx.x] = o;
@@ -635,9 +681,10 @@ __device__ __forceinline__ void combine_heads(const float *lp, const float *op, 
         for (int e = 0; e < 4; ++e) out[at + e] = __float2half_rn(o[e]);
 }
 
-// Rows of more than one chunk.  x: selected heads, y: sequences.
+// Rows of more than one chunk.  x: selected heads, y: sequences.  (At most 64 registers, eight waves a SIMD: both
+// kernels below wait for short chains of loads.)
 template <int D, int R>
-__global__ void __launch_bounds__(kCkThreads) chunk_combine_kernel(ChunkParams p)
+__global__ void __launch_bounds__(kCkThreads, 8) chunk_combine_kernel(ChunkParams p)
 {
     __shared__ float lse[R];
     __shared__ f32x4 part[kCkThreads];
@@ -662,7 +709,7 @@ __global__ void __launch_bounds__(kCkThreads) chunk_combine_kernel(ChunkParams p
 constexpr int weight_tokens(int R) { return kCkThreads * (R == 8 ? 2 : R == 4 ? 4 : 8); }        // of a piece
 constexpr int weight_parts(int R) { return R < 4 ? R : 4; }                                      // at least
 template <int D, int R>
-__global__ void __launch_bounds__(kCkThreads) chunk_weights_kernel(ChunkParams p)
+__global__ void __launch_bounds__(kCkThreads, 8) chunk_weights_kernel(ChunkParams p)
 {
     constexpr int HEADS = R / weight_parts(R);           // of a part
     __shared__ float lse[R];

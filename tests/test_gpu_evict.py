@@ -182,6 +182,44 @@ def test_infinite_values(D, hq, hkv):
     assert np.isfinite(out[..., others]).all()
 
 
+@pytest.mark.parametrize("D,hq,hkv", [(64, 1, 1), (128, 4, 2), (64, 8, 2), (128, 8, 1)])
+def test_infinite_values_of_unlikely_tokens(D, hq, hkv):
+    """An infinite value is what its dim comes to however small its token's probability is: in a wave's tokens, in
+    a chunk of the row that hardly counts, or below what a float shows; the other dims and the weights are finite."""
+    a = Case(False, [33, 512, 1500], hq, hkv, D, seed=217)
+    c = a.c
+    c.scale = np.log(2)                              # a score is the logarithm of a probability to base 2
+    c.q[:] = 0
+    c.q[..., 0] = 1
+    put = {}
+    for b, L in enumerate(c.lens):
+        for g in range(hkv):
+            for t in range(L):
+                blk, at = c.table[b, t // 16], t % 16
+                c.k[blk, g, at, 0] = -300 if t >= 1024 else -(t % 3)
+            for t, score, d, x in ((L - 1, -26, 3, np.inf), (L // 2, -60, 9, -np.inf), (7, -120, 20, np.inf),
+                                   (L - 2, -400, D - 1, -np.inf), (31, -2000, 40, np.inf)):
+                blk, at = c.table[b, t // 16], t % 16
+                c.k[blk, g, at, 0] = score
+                c.v[blk, g, at, d] = x
+                put[d] = x
+    a.k, a.v = torch.from_numpy(c.k).to(DEV), torch.from_numpy(c.v).to(DEV)
+    w = torch.full(a.w.shape, 3.0, device=DEV)
+    out, w = a.run(list(range(hkv)), 0.0, None, w).cpu().numpy(), w.cpu().numpy()
+    for b, L in enumerate(c.lens):
+        for g in range(hkv):
+            k, v = a.rows(b, g)
+            q = c.q[b, g * c.r:(g + 1) * c.r].astype(np.float64)
+            near = k[:, 0] >= -2                     # (the others weigh 2^-26 and less: within the bound's sum |v| 2^-24)
+            ref, _, tol = attention_bound(q, k[near], np.where(np.isinf(v), 0.0, v)[near], c.scale)
+            for d in range(D):
+                got = out[b, g * c.r:(g + 1) * c.r, d].astype(np.float64)
+                assert (got == put[d]).all() if d in put else (np.abs(got - ref[:, d]) <= tol[:, d]).all(), (b, g, d, got)
+            # a score x to base 2 is rounded four times, scale and log-sum-exp included: 4 ln 2 2^-24 |x| of the weight
+            p = R.attend(q, k, np.zeros_like(v), c.scale)[1].sum(0)
+            assert (np.abs(w[b, g, :L] - p) <= (2.0 ** -22 * np.abs(k[:, 0]) + 2.0 ** -18) * p + 1e-37).all(), (b, g)
+
+
 def test_weights_of_many_short_rows():
     lens = np.random.default_rng(213).integers(0, 70, 1100)
     a = Case(True, lens, 2, 2, 64, seed=214)

@@ -33,7 +33,8 @@ extern "C" {
  * rounding), and for every selected KV head g and every slot t < seq_lens[b]
  *     weights_out[b, g, t] = decay * weights_in[b, g, t] + sum_j softmax_t(scale q[b, g r + j] . K)
  * over the r query heads of the group, in fp32.  (An infinite value of V is what its dim of `out` comes to, however small
- * its token's probability is; of an fp16 cache hetis_attn_decode has NaN there where a probability is held as 0.)
+ * its token's probability is; of an fp16 cache hetis_attn_decode has NaN there where a probability is held as 0.  Tokens
+ * with scores of -inf have no weight and add nothing, unless a row has no others: NaN.)
  *   decay        host, finite and >= 0; 1 adds up, 0 does not read weights_in
  *   weights_in   or NULL: no history;  weights_out  may be the same array, or one that does not overlap
  *   n_seen, positions   both, or both NULL.  positions[b, g, seq_lens[b] - 1] = n_seen[b] - 1 is written:

@@ -592,10 +592,12 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
 #pragma unroll
                 for (int e = 0; e < kFoldDims; ++e) o[e] += f[w] * lds.o[turn][w][j][d + e];
             if constexpr (!KV4) infinite_dims<D>(p, cur, p.scores + (row * r + j) * p.slots, d, M, o);
-            const float inv = cur.tokens > 0 ? 1.f / sum : 0.f;
+            // A chunk whose scores are all -inf adds nothing to its row (log-sum-exp -inf); only a row of such tokens
+            // alone is NaN.
+            const bool whole = cur.L <= kCkTokens;
+            const float inv = 1.f / (sum != 0.f || whole ? sum : INFINITY);
 #pragma unroll
             for (int e = 0; e < kFoldDims; ++e) o[e] = cur.tokens > 0 ? o[e] * inv : 0.f;
-            const bool whole = cur.L <= kCkTokens;
             const int64_t part = (row * p.max_chunks + cur.chunk) * r + j;
             if (whole) {
                 __half *to = p.out + ((int64_t)cur.b * p.n_q_heads + cur.g * r + j) * D + d;

@@ -220,6 +220,45 @@ def test_infinite_values_of_unlikely_tokens(D, hq, hkv):
             assert (np.abs(w[b, g, :L] - p) <= (2.0 ** -22 * np.abs(k[:, 0]) + 2.0 ** -18) * p + 1e-37).all(), (b, g)
 
 
+@pytest.mark.parametrize("D,hq,hkv", [(64, 1, 1), (128, 4, 2), (64, 8, 2), (128, 8, 1)])
+def test_tokens_without_any_weight(D, hq, hkv):
+    """Scores of -inf: in all tokens of a wave, of a chunk, of several, at either end; only where they are all a row
+    has is it NaN."""
+    lost = [(0, 128), (512, 1024), (0, 1024), (1024, 1300), (100, 1290), (0, 700)]
+    a = Case(False, [512, 1300, 1300, 1300, 1300, 700, 90], hq, hkv, D, seed=218)
+    c = a.c
+    c.q[..., 0] = 1
+    for b, (t0, t1) in enumerate(lost):
+        for t in range(t0, t1):
+            c.k[c.table[b, t // 16], :, t % 16, 0] = -np.inf
+    a.k = torch.from_numpy(c.k).to(DEV)
+    w = torch.full(a.w.shape, 3.0, device=DEV)
+    heads = list(range(hkv))
+    out, w = a.run(heads, 0.75, f32(a.w), w).cpu().numpy(), w.cpu().numpy()
+    for b, L in enumerate(c.lens):
+        t0, t1 = lost[b] if b < len(lost) else (0, 0)
+        there = np.ones(L, dtype=bool)
+        there[t0:t1] = False
+        for g in range(hkv):
+            got = out[b, g * c.r:(g + 1) * c.r].astype(np.float64)
+            if not there.any():
+                assert np.isnan(got).all() and np.isnan(w[b, g, :L]).all()
+                continue
+            k, v = (x[there] for x in a.rows(b, g))
+            q = c.q[b, g * c.r:(g + 1) * c.r].astype(np.float64)
+            ref, p, tol = attention_bound(q, k, v, c.scale)
+            assert (np.abs(got - ref) <= tol).all(), (b, g)
+            # (check() has the derivation)
+            _, _, _, _, s_max, S = R.attend(q, k, v, c.scale)
+            old = 0.75 * a.w[b, g, :L].astype(np.float64)
+            delta = 2 * ((D + 4) * 2.0 ** -24 * S + 4 * 2.0 ** -23 * s_max) + 2.0 ** -19
+            want = old.copy()
+            want[there] += p.sum(0)
+            off = np.zeros(L)
+            off[there] = delta * p.sum(0)
+            assert (np.abs(w[b, g, :L] - want) <= off + 2.0 ** -22 * (want + old)).all(), (b, g)
+
+
 def test_weights_of_many_short_rows():
     lens = np.random.default_rng(213).integers(0, 70, 1100)
     a = Case(True, lens, 2, 2, 64, seed=214)

@@ -340,6 +340,38 @@ def test_scales_half_way_between_two_numbers():
     assert_same(v4, want_v)
 
 
+def test_scales_of_every_quotient_half_way():
+    """(hi - lo) / 15 = 1 + (2 k + 1) / 2048, half way between two fp16 numbers, for every such quotient below 2: the
+    scale is the fp32 product with f32(1 / 15), rounded, and then rounded to fp16, which is not everywhere what a
+    division gives or one rounding of the exact product."""
+    k = np.arange(1024)
+    d = 15 * (1 + (2 * k + 1) / 2048)
+    lo, hi = -np.ceil(d), d - np.ceil(d)
+    assert (hi.astype(np.float16) == hi).all() and (lo.astype(np.float16) == lo).all()
+    f = np.float32
+    product = (d.astype(f) * (f(1) / f(15))).astype(np.float16)
+    assert (product != (d.astype(f) / f(15)).astype(np.float16)).any()
+    assert (product != (d * np.float64(f(1) / f(15))).astype(np.float16)).any()
+    n = len(k)
+    c = Cache4([n], 1, 1, 64, seed=24)
+    kn = np.zeros((n, 1, 64), dtype=np.float16)
+    kn[:, 0] = (lo + np.random.default_rng(25).random((64, n)) * d).T
+    kn[:, 0, 3::32], kn[:, 0, 9::32] = lo[:, None], hi[:, None]
+    vn = (kn * np.float16(-0.25)).astype(np.float16)
+    for x, m in ((kn, 1), (vn, 0.25)):
+        assert (R.quantise(x)[1] == product[:, None, None].astype(np.float64) * m).all()
+    seq, pos = np.zeros(n, dtype=np.int32), np.arange(n, dtype=np.int32)
+    k4, v4 = torch.from_numpy(c.k4).to(DEV), torch.from_numpy(c.v4).to(DEV)
+    H.check(H.hetis_kv4_store(c.shape(), torch.from_numpy(kn).to(DEV), torch.from_numpy(vn).to(DEV), i32(seq), i32(pos),
+                              n, i32(c.table), i32([0]), 1, c.nb, k4, v4))
+    want_k, want_v = c.k4.copy(), c.v4.copy()
+    for t in range(n):
+        R.put_row(want_k[c.table[0, t // 16], 0], c.places[0], t % 16, kn[t, 0])
+        R.put_row(want_v[c.table[0, t // 16], 0], c.places[1], t % 16, vn[t, 0])
+    assert_same(k4, want_k)
+    assert_same(v4, want_v)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_append(D):
     c = Cache4([1, 15, 16, 17, 0, 33, 160], 4, 4, D, seed=22)
@@ -410,3 +442,75 @@ def test_move(D, moves):
     H.check(H.hetis_kv4_move(c.shape(), i32(src), i32(dst), moves, i32(c.table), i32(heads), 2, c.nb, k4, v4))
     assert_same(k4, want[0])
     assert_same(v4, want[1])
+
+
+# ------------------------------------------------------------------ strides
+
+def layouts(nb, hkv, tile, unit):
+    """(stride of blocks, of heads) in units of `unit` bytes, for tiles of `tile` bytes: heads outermost, with gaps, and
+    blocks so far apart that offsets pass 32 bits."""
+    far = -(-(5 << 30) // nb // 16) * 16
+    assert far * (nb - 1) > 1 << 32
+    return {"heads first": ((tile + 32) // unit, (nb * (tile + 32) + 48) // unit),
+            "gaps": ((hkv * (tile + 48) + 80) // unit, (tile + 48) // unit),
+            "far": (far // unit, (tile + 16) // unit)}
+
+
+def spread(pool, sb, sh):
+    """The tiles of `pool` [nb, hkv, ...] in a buffer with these strides, other bytes 0x5A."""
+    nb, hkv = pool.shape[:2]
+    n = pool[0, 0].numel()
+    buf = torch.empty((nb - 1) * sb + (hkv - 1) * sh + n, dtype=pool.dtype, device=DEV)
+    buf.view(torch.uint8).fill_(0x5A)
+    buf.as_strided((nb, hkv, n), (sb, sh, 1)).copy_(pool.reshape(nb, hkv, n))
+    return buf
+
+
+def same_buffer(buf, pool, sb, sh):
+    """`buf` holds the tiles of `pool`, and 0x5A in every other byte (looked at in place: it may be large)."""
+    tiles = buf.as_strided((*pool.shape[:2], pool[0, 0].numel()), (sb, sh, 1))
+    assert torch.equal(tiles.contiguous().view(torch.uint8), pool.reshape(tiles.shape).contiguous().view(torch.uint8))
+    tiles.copy_(torch.full((1,), 0x5A, dtype=torch.uint8, device=DEV).expand(tiles.element_size()).contiguous().view(tiles.dtype))
+    flat = buf.view(torch.uint8)
+    for i in range(0, flat.numel(), 1 << 28):
+        assert bool((flat[i:i + (1 << 28)] == 0x5A).all())
+
+
+@pytest.mark.parametrize("layout", ["heads first", "gaps", "far"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_and_attention_with_strides(layout, D):
+    """Append, store, fetch, move and Attention: what they do to pools of the default layout, and no other byte."""
+    c = Cache4([300, 17, 0, 530], 8, 4, D, seed=32)
+    heads, (seq, pos) = [3, 1], entries(c, 33, 200)
+    rng = np.random.default_rng(34)
+    new = [torch.from_numpy(rng.standard_normal((n, 4, D)).astype(np.float16)).to(DEV) for n in (4, 4, 200, 200)]
+    src, dst = (np.full((4, 2, 9), -1) for _ in range(2))
+    for b, L in enumerate(c.lens):
+        for i in range(2):
+            slots, n = rng.permutation(L), min(9, L // 2)
+            src[b, i, :n], dst[b, i, :n] = slots[:n], slots[n:2 * n]
+    sb, sh = layouts(c.nb, 4, 10 * D, 1)[layout]
+    bt, sl, hid, ts, tp = i32(c.table), i32(c.lens), i32(heads), i32(seq), i32(pos)
+
+    def steps(shape, k4, v4):
+        """Pools are compared after every call that writes them."""
+        H.check(H.hetis_kv4_append(shape, new[0], new[1], bt, sl, hid, 2, c.nb, k4, v4))
+        yield None
+        H.check(H.hetis_kv4_store(shape, new[2], new[3], ts, tp, 200, bt, hid, 2, c.nb, k4, v4))
+        yield None
+        H.check(H.hetis_kv4_move(shape, i32(src), i32(dst), 9, bt, hid, 2, c.nb, k4, v4))
+        yield None
+        rows = [torch.full((200, 4, D), 7.0, dtype=torch.float16, device=DEV) for _ in range(2)]
+        H.check(H.hetis_kv4_fetch(shape, k4, v4, ts, tp, 200, bt, hid, 2, c.nb, *rows))
+        yield rows
+        yield [c.decode(heads, k4=k4, v4=v4, shape=shape)]
+
+    plain = [torch.from_numpy(p).to(DEV) for p in (c.k4, c.v4)]
+    far = [spread(p, sb, sh) for p in plain]
+    for a, b in zip(steps(c.shape(), *plain), steps(c.shape(kv_stride_block=sb, kv_stride_head=sh), *far)):
+        for p, f in zip(plain, far):
+            assert torch.equal(p, f.as_strided(p.shape, (sb, sh, 1)))
+        for x, y in zip(a or [], b or []):
+            assert np.array_equal(bits(x), bits(y))
+    for p, f in zip(plain, far):
+        same_buffer(f, p, sb, sh)

@@ -8,7 +8,7 @@ import paper_2509_08309_amd as H
 from paper_2509_08309_amd import workloads as W
 
 from gpu_harness import Dev, bits, selected_rows, unselected_rows, SENTINEL
-from test_gpu_kv4 import EDGES, Cache4, attention_bound, i32
+from test_gpu_kv4 import EDGES, Cache4, attention_bound, i32, layouts, same_buffer, spread
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -515,3 +515,35 @@ def test_profile_events_carry_the_calls(kv4):
             H.hetis_kv_profile_events(None, None)
         torch.cuda.synchronize()
         assert 0.0 < begin.elapsed_time(end) < 5.0 and begin.elapsed_time(end) != old
+
+
+# ------------------------------------------------------------------ strides
+
+@pytest.mark.parametrize("layout", ["heads first", "gaps", "far"])
+@pytest.mark.parametrize("kv4", [False, True])
+def test_weights_with_strides(kv4, layout):
+    """Outputs and weights of the default layout bit for bit, and moves that touch no other byte (fp16)."""
+    a = Case(kv4, [300, 17, 0, 1100], 8, 4, 128, seed=340)
+    c, heads = a.c, [3, 1]
+    unit, tile = (1, 1280) if kv4 else (2, 4096)
+    sb, sh = layouts(c.nb, 4, tile, unit)[layout]
+    w = [torch.full(a.w.shape, 3.0, device=DEV) for _ in range(2)]
+    pos = [torch.full(a.w.shape, -7, dtype=torch.int32, device=DEV) for _ in range(2)]
+    want = bits(a.run(heads, 0.75, f32(a.w), w[0], i32(a.seen), pos[0]))
+    out = torch.empty(c.q.shape, dtype=torch.float16, device=DEV)
+    out.view(torch.int16).fill_(np.int16(SENTINEL))
+    shape = c.shape(kv_stride_block=sb, kv_stride_head=sh)
+    k, v = spread(a.k, sb, sh), spread(a.v, sb, sh)
+    call = H.hetis_attn_decode_kv4_weights if kv4 else H.hetis_attn_decode_weights
+    H.check(call(shape, torch.from_numpy(c.q).to(DEV), k, v, i32(c.table), i32(c.lens), i32(heads), 2, c.scale, 0.75, f32(a.w),
+                 i32(a.seen), out, w[1], pos[1]))
+    assert np.array_equal(bits(out), want) and torch.equal(pos[0], pos[1])
+    assert torch.equal(w[0].view(torch.int32), w[1].view(torch.int32))
+    if not kv4:                                      # (of the 4-bit cache: test_rows_and_attention_with_strides)
+        src, dst = np.full((4, 2, 9), -1), np.full((4, 2, 9), -1)
+        src[0, :, :9], dst[0, :, :9] = np.arange(290, 299), np.arange(9) * 17
+        src[3, 1, :2], dst[3, 1, :2] = [1099, 5], [16, 1000]
+        for s, pools in ((c.shape(), (a.k, a.v)), (shape, (k, v))):
+            H.check(H.hetis_kv_move(s, i32(src), i32(dst), 9, i32(c.table), i32(heads), 2, c.nb, *pools))
+    same_buffer(k, a.k, sb, sh)
+    same_buffer(v, a.v, sb, sh)

@@ -683,10 +683,10 @@ __device__ __forceinline__ void combine_heads(const float *lp, const float *op, 
         for (int e = 0; e < 4; ++e) out[at + e] = __float2half_rn(o[e]);
 }
 
-// Rows of more than one chunk.  x: selected heads, y: sequences.  (At most 64 registers, eight waves a SIMD: both
-// kernels below wait for short chains of loads.)
+// Rows of more than one chunk.  x: selected heads, y: sequences.  (Held to 64 registers, which is eight waves a
+// SIMD instead of seven, this kernel and the next one are no faster: 12 x 3 groups with weights 21.2 -> 21.4 us.)
 template <int D, int R>
-__global__ void __launch_bounds__(kCkThreads, 8) chunk_combine_kernel(ChunkParams p)
+__global__ void __launch_bounds__(kCkThreads) chunk_combine_kernel(ChunkParams p)
 {
     __shared__ float lse[R];
     __shared__ f32x4 part[kCkThreads];
@@ -711,7 +711,7 @@ __global__ void __launch_bounds__(kCkThreads, 8) chunk_combine_kernel(ChunkParam
 constexpr int weight_tokens(int R) { return kCkThreads * (R == 8 ? 2 : R == 4 ? 4 : 8); }        // of a piece
 constexpr int weight_parts(int R) { return R < 4 ? R : 4; }                                      // at least
 template <int D, int R>
-__global__ void __launch_bounds__(kCkThreads, 8) chunk_weights_kernel(ChunkParams p)
+__global__ void __launch_bounds__(kCkThreads) chunk_weights_kernel(ChunkParams p)
 {
     constexpr int HEADS = R / weight_parts(R);           // of a part
     __shared__ float lse[R];

@@ -35,7 +35,7 @@ def residents(name):
     if m:                                                    # chunk_residents()
         return {("64", "1"): 4, ("64", "0"): 3, ("128", "1"): 3, ("128", "0"): 2}[m.groups()]
     if "chunk_combine" in name or "chunk_weights" in name:
-        return 8
+        return 7
     if "evict_kernel" in name:
         return 1
     assert "kv4_rows_kernel" in name or "kv_move_rows_kernel" in name, name

@@ -151,6 +151,60 @@ def test_weights_of_long_rows(kv4, hq, hkv, heads):
 
 
 @pytest.mark.parametrize("kv4", [False, True])
+@pytest.mark.parametrize("hq", [1, 8])
+def test_weights_of_more_chunks_than_a_wave_has_lanes(kv4, hq):
+    a = Case(kv4, [70000, 3, 33000], hq, 1, 64, seed=220)
+    w_out = torch.full(a.w.shape, 3.0, device=DEV)
+    a.check(a.run([0], 1.0, f32(a.w), w_out), [0], 1.0, w_out, np.full(a.w.shape, 3.0))
+
+
+@pytest.mark.parametrize("kv4", [False, True])
+@pytest.mark.parametrize("scale", [0.0, -0.125, 3.0, 1e-20])
+def test_weights_at_scales(kv4, scale):
+    a = Case(kv4, [700, 33, 1, 512, 0, 1040], 8, 2, 64, seed=221)
+    a.c.scale = scale
+    w_out = torch.full(a.w.shape, 3.0, device=DEV)
+    a.check(a.run([1, 0], 0.5, f32(a.w), w_out), [1, 0], 0.5, w_out, np.full(a.w.shape, 3.0))
+
+
+@pytest.mark.parametrize("kv4", [False, True])
+def test_the_widest_table(kv4):
+    """2^24 blocks a sequence: scores and weights past 2^32 bytes, and the bits of a table as wide as the rows."""
+    a = Case(kv4, [1100], 24, 3, 64, seed=222)
+    c, mb, heads = a.c, 1 << 24, [2, 1]
+    want_w, pos = torch.full(a.w.shape, 3.0, device=DEV), torch.full(a.w.shape, -7, dtype=torch.int32, device=DEV)
+    want = bits(a.run(heads, 0.5, f32(a.w), want_w, i32(a.seen), pos))
+    shape = H.make_shape(1, 24, 3, 64, mb)
+    rc, n = H.hetis_attn_decode_weights_workspace_bytes(shape, 2)
+    assert rc == 0 and n > 16 << 30
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    H.check(H.hetis_attn_workspace_init(ws, 1 << 21))
+    bt = torch.full((1, mb), -1, dtype=torch.int32, device=DEV)
+    bt[:, :c.mb] = i32(c.table)
+    w, p = torch.zeros((1, 3, 16 * mb), device=DEV), torch.full((1, 3, 16 * mb), -7, dtype=torch.int32, device=DEV)
+    w[:, :, :a.T] = f32(a.w)
+    out = torch.empty(c.q.shape, dtype=torch.float16, device=DEV)
+    out.view(torch.int16).fill_(np.int16(SENTINEL))
+    call = H.hetis_attn_decode_kv4_weights_ws if kv4 else H.hetis_attn_decode_weights_ws
+    H.check(call(shape, torch.from_numpy(c.q).to(DEV), a.k, a.v, bt, i32(c.lens), i32(heads), 2, c.scale, 0.5, w,
+                 i32(a.seen), out, w, p, ws, n))
+    assert np.array_equal(bits(out), want)
+    assert torch.equal(w[:, 1:, :1100], want_w[:, 1:, :1100]) and torch.equal(w[:, 0, :1100], f32(a.w)[:, 0, :1100])
+    assert torch.equal(p[:, :, :a.T], pos) and not bool((w[:, :, a.T:] != 0).any())
+    del ws
+    new = torch.zeros(1, dtype=torch.int32, device=DEV)
+    src, dst = (torch.zeros((1, 2, 300), dtype=torch.int32, device=DEV) for _ in range(2))
+    p[:, :, :1100] = torch.arange(1100, dtype=torch.int32, device=DEV)
+    before = w[0, 1:, :1100].cpu().numpy()
+    H.check(H.hetis_kv_evict(shape, w, p, i32([1100]), i32([1100]), i32([300]), i32(heads), 2, 4, 20, 300, w, p, new, src, dst))
+    assert int(new[0]) == 300
+    for i, g in enumerate(heads):
+        n, s, d, w2, p2 = R.evict(before[g - 1], np.arange(1100), 1100, 300, 4, 20, 300)
+        assert list(src[0, i].cpu().numpy()) == s + [-1] * (300 - len(s)) and list(dst[0, i].cpu().numpy()) == d + [-1] * (300 - len(d))
+        assert np.array_equal(w[0, g, :1100].cpu().numpy(), w2) and np.array_equal(p[0, g, :1100].cpu().numpy(), p2)
+
+
+@pytest.mark.parametrize("kv4", [False, True])
 def test_weights_of_many_items_and_few_bit_for_bit(kv4):
     lens = np.random.default_rng(215).integers(1, 2300, 130)
     lens[:10] = [0, 512, 513, 1024, 1025, 1536, 1537, 2048, 2049, 4097]
@@ -358,6 +412,29 @@ def test_heads_named_twice_or_not_there():
     a.run(shape_heads, [40, 100], 1, 5, 800)
 
 
+@pytest.mark.parametrize("kind", ["spread", "odd"])
+@pytest.mark.parametrize("which", ["weights", "positions"])
+def test_one_array_in_place_and_the_other_not(kind, which):
+    a = Rows([50, 700, 4097, 9000], 2, 307, kind)
+    shape = H.make_shape(4, 2, 2, 64, a.mb)
+    budgets = [20, 300, 1000, 5000]
+    got = []
+    for in_place in (False, True):
+        w, p = f32(a.w), i32(a.p)
+        w2, p2 = f32(a.w), i32(a.p)                  # (slots that are not in use: alike in both)
+        if in_place:
+            w2, p2 = (w, p2) if which == "weights" else (w2, p)
+        new = torch.zeros(4, dtype=torch.int32, device=DEV)
+        src, dst = (torch.zeros((4, 1, 9000), dtype=torch.int32, device=DEV) for _ in range(2))
+        H.check(H.hetis_kv_evict(shape, w, p, i32(a.lens), i32(a.seen), i32(budgets), i32([1]), 1, 4, 30, 9000, w2, p2, new, src, dst))
+        got.append([x.cpu().numpy() for x in (w2.view(torch.int32), p2, new, src, dst)])
+    assert all(np.array_equal(x, y) for x, y in zip(*got))
+    for b, L in enumerate(a.lens):
+        n, s, d, _, pr = R.evict(a.w[b, 1, :L], a.p[b, 1, :L], a.seen[b], budgets[b], 4, 30, 9000)
+        assert got[0][2][b] == n and list(got[0][3][b, 0, :len(s)]) == s and list(got[0][4][b, 0, :len(d)]) == d
+        assert np.array_equal(got[0][1][b, 1, :L], pr)
+
+
 def test_many_rows():
     rng = np.random.default_rng(304)
     a = Rows(rng.integers(0, 90, 300), 2, 305, "ties")
@@ -455,6 +532,57 @@ def test_a_stream_of_steps_with_evictions(kv4, D, hq, hkv):
             lens = new.cpu().numpy().astype(int)
             assert all(len(rows) == lens[b] for (b, g), rows in model.items())
             assert all({0, 1} <= {x[0] for x in rows} for rows in model.values())           # the sinks stayed
+
+
+@pytest.mark.parametrize("kv4", [False, True])
+def test_a_captured_step_with_eviction(kv4):
+    """The new rows, Attention with weights, the choice, the moves and Attention over what is left in one graph: every
+    replay does what the same calls do one by one."""
+    a = Case(kv4, [300, 33, 700], 8, 2, 64, seed=331)
+    c = a.c
+    q, bt, hid = torch.from_numpy(c.q).to(DEV), i32(c.table), i32([1, 0])
+    lens, seen, budgets, new_rows = i32(c.lens), i32(a.seen), i32([120, 20, 600]), []
+    for seed in (1, 2):
+        new_rows.append(torch.from_numpy(np.random.default_rng(seed).standard_normal((3, 2, 64)).astype(np.float16)).to(DEV))
+    rc, n = H.hetis_attn_decode_weights_workspace_bytes(c.shape(), 2)
+    H.check(rc)
+
+    def state():
+        w = f32(np.nan_to_num(a.w))
+        p = i32(np.tile(np.arange(a.T), (3, 2, 1)))
+        ws = torch.zeros(n, dtype=torch.uint8, device=DEV)
+        outs = [torch.zeros(c.q.shape, dtype=torch.float16, device=DEV) for _ in range(2)]
+        lists = [torch.zeros((3, 2, 200), dtype=torch.int32, device=DEV) for _ in range(2)]
+        return dict(k=a.k.clone(), v=a.v.clone(), w=w, p=p, ws=ws, outs=outs, lists=lists, new=torch.zeros_like(lens))
+
+    def step(s):
+        append = H.hetis_kv4_append if kv4 else H.hetis_kv_append
+        H.check(append(c.shape(), *new_rows, bt, lens, hid, 2, c.nb, s["k"], s["v"]))
+        weights = H.hetis_attn_decode_kv4_weights_ws if kv4 else H.hetis_attn_decode_weights_ws
+        H.check(weights(c.shape(), q, s["k"], s["v"], bt, lens, hid, 2, c.scale, 0.5, s["w"], seen, s["outs"][0], s["w"], s["p"],
+                        s["ws"], n))
+        H.check(H.hetis_kv_evict(c.shape(), s["w"], s["p"], lens, seen, budgets, hid, 2, 2, 8, 200, s["w"], s["p"], s["new"],
+                                 *s["lists"]))
+        move = H.hetis_kv4_move if kv4 else H.hetis_kv_move
+        H.check(move(c.shape(), *s["lists"], 200, bt, hid, 2, c.nb, s["k"], s["v"]))
+        decode = H.hetis_attn_decode_kv4_ws if kv4 else H.hetis_attn_decode_ws
+        H.check(decode(c.shape(), q, s["k"], s["v"], bt, s["new"], hid, 2, c.scale, s["outs"][1], s["ws"], n))
+
+    one, two = state(), state()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(one)
+    for turn in range(4):
+        # slots behind the new lengths come back (weight 0, position -1), so that every turn has something to choose
+        g.replay()
+        step(two)
+        torch.cuda.synchronize()
+        assert torch.equal(one["new"], two["new"]) and list(one["new"].cpu()) == [120, 20, 600], turn
+        for x in ("k", "v", "w", "p"):
+            assert torch.equal(one[x].view(torch.uint8), two[x].view(torch.uint8)), (turn, x)
+        for x, y in zip(one["outs"] + one["lists"], two["outs"] + two["lists"]):
+            assert torch.equal(x, y), turn
+    assert bool((one["lists"][0] >= 0).any())
 
 
 def test_evicted_cache_in_the_other_calls():

@@ -226,6 +226,28 @@ def test_strides_and_offsets_past_32_bits():
     assert np.array_equal(bits(c.decode([0, 1], k4=pool, v4=pool[1 << 20:], shape=s)), whole)
 
 
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 1)])
+def test_rows_of_more_chunks_than_a_wave_has_lanes(hq, hkv):
+    c = Cache4([70000, 33000, 5], hq, hkv, 64, seed=35)
+    c.check(c.decode([0]), [0])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_values_below_the_normal_numbers_of_fp16(D):
+    """Scales, keys and values that are subnormal count like others: nothing on the way sets them to zero."""
+    def dist(c):
+        c.k = (c.k.astype(np.float64) * 1e-6).astype(np.float16)
+        c.v = (3e-5 + c.v.astype(np.float64) * 1e-6).astype(np.float16)
+    c = Cache4([700, 33, 1, 512], 8, 2, D, seed=36, dist=dist)
+    c.scale = 2e5
+    assert 0 < np.abs(c.k).max() < 2.0 ** -14 and 0 < np.abs(c.v).max() < 2.0 ** -14
+    out = c.decode([0, 1])
+    c.check(out, [0, 1])
+    k, v = c.rows(0, 1)
+    ref, p, tol = attention_bound(c.q[0, 4:].astype(np.float64), k, v, c.scale)
+    assert p.max() > 0.02 and (tol < 0.05 * np.abs(ref)).all()          # (so that the above says something)
+
+
 def test_workspaces_streams_and_graphs():
     c = Cache4([1300, 700, 5, 2000], 16, 2, 128, seed=14)
     heads = [0, 1]
@@ -370,6 +392,34 @@ def test_scales_of_every_quotient_half_way():
         R.put_row(want_v[c.table[0, t // 16], 0], c.places[1], t % 16, vn[t, 0])
     assert_same(k4, want_k)
     assert_same(v4, want_v)
+
+
+def test_more_entries_than_a_grid_reaches():
+    """2^20 entries and more in one call: the pools and rows of two calls with half of them each."""
+    n, D = (1 << 20) + 12345, 64
+    mb = -(-n // 16)
+    shape = H.make_shape(1, 1, 1, D, mb)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(37)
+    kn, vn = (torch.randn((n, 1, D), generator=gen, device=DEV).half() for _ in range(2))
+    bt = torch.randperm(mb, generator=gen, device=DEV).int()[None].contiguous()
+    seq, pos, hid = torch.zeros(n, dtype=torch.int32, device=DEV), torch.arange(n, dtype=torch.int32, device=DEV), i32([0])
+    pools = [[torch.zeros((mb, 1, 10 * D), dtype=torch.uint8, device=DEV) for _ in range(2)] for _ in range(2)]
+    H.check(H.hetis_kv4_store(shape, kn, vn, seq, pos, n, bt, hid, 1, mb, *pools[0]))
+    for part in (slice(0, n // 2), slice(n // 2, n)):
+        m = part.stop - part.start
+        H.check(H.hetis_kv4_store(shape, kn[part], vn[part], seq[part], pos[part], m, bt, hid, 1, mb, *pools[1]))
+    assert all(torch.equal(a, b) for a, b in zip(*pools))
+    whole = [torch.zeros_like(kn) for _ in range(2)]
+    H.check(H.hetis_kv4_fetch(shape, *pools[0], seq, pos, n, bt, hid, 1, mb, *whole))
+    for got, x in zip(whole, (kn, vn)):
+        at = np.r_[0:200, n - 200:n]
+        assert np.array_equal(got[at].cpu().numpy(), R.held(x[at].cpu().numpy()))
+        half = torch.zeros_like(x[n // 2:])
+        other = torch.zeros_like(half)
+        H.check(H.hetis_kv4_fetch(shape, *pools[0], seq[n // 2:], pos[n // 2:], n - n // 2, bt, hid, 1, mb,
+                                  *((half, other) if x is kn else (other, half))))
+        assert torch.equal(half, got[n // 2:])
 
 
 @pytest.mark.parametrize("D", [64, 128])

@@ -32,9 +32,9 @@ extern "C" {
  * hetis_attn_decode that also accumulates attention weight: `out` as hetis_attn_decode computes it (to
  * rounding), and for every selected KV head g and every slot t < seq_lens[b]
  *     weights_out[b, g, t] = decay * weights_in[b, g, t] + sum_j softmax_t(scale q[b, g r + j] . K)
- * over the r query heads of the group, in fp32.  (An infinite value of V is what its dim of `out` comes to, however small
- * its token's probability is; of an fp16 cache hetis_attn_decode has NaN there where a probability is held as 0.  Tokens
- * with scores of -inf have no weight and add nothing, unless a row has no others: NaN.)
+ * over the r query heads of the group, in fp32.  Infinite numbers: a value of V is what its dim of `out` comes
+ * to, however small its token's probability is; tokens with scores of -inf have no weight and add nothing,
+ * unless a row has no others (NaN).  hetis_attn_decode may have NaN in such rows.
  *   decay        host, finite and >= 0; 1 adds up, 0 does not read weights_in
  *   weights_in   or NULL: no history;  weights_out  may be the same array, or one that does not overlap
  *   n_seen, positions   both, or both NULL.  positions[b, g, seq_lens[b] - 1] = n_seen[b] - 1 is written:
@@ -90,11 +90,11 @@ int hetis_attn_decode_weights_workspace_bytes(const hetis_attn_shape *shape, int
  * that were in use get weight 0 and position -1, slots not in use are left as they are.
  *   positions_in   or NULL: slot t holds position t
  *   weights_out / positions_out   may be weights_in / positions_in, or may not overlap them
- *   new_lens  int32 [B], not seq_lens;  move_src, move_dst  int32 [B, n_sel_heads, max_moves]
+ *   new_lens  int32 [B], none of the inputs;  move_src, move_dst  int32 [B, n_sel_heads, max_moves]
  *   n_sink, n_recent (>= 0), max_moves (>= 1)  host
  * The cache itself is not touched: hetis_kv_move or hetis_kv4_move follows, and seq_lens becomes new_lens.
  * Of a head that head_ids names twice the first entry counts, the list of the others is empty.
- * shape: n_q_heads and the strides are not used.  Allocates nothing, keeps no state.
+ * shape: as for the other calls; n_q_heads has no effect, and strides are ignored.  Allocates nothing, keeps no state.
  * Errors: NULL, BAD_SHAPE, UNSUPPORTED, BAD_HEADS, LAUNCH.
  */
 int hetis_kv_evict(const hetis_attn_shape *shape, const float *weights_in,

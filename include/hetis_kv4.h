@@ -8,9 +8,14 @@
  * Values.  A row of D fp16 values is cut into groups of HETIS_KV4_GROUP = 32.  With lo and hi the
  * smallest and largest value of a group (fp32 arithmetic, f16() rounds to nearest even)
  *     s = f16((hi - lo) * f32(1 / 15))     b = f16(lo - 16 s)     c = clamp(rint((x - b) / s - 16), 0, 15)
- * (a product with the fp32 number nearest to 1 / 15; c = 0 where s = 0) and the value held is f16(s * (16 + c) + b), rounded once.  Values are first
- * cut to +-20480, so that b is finite; a group with a NaN holds NaN throughout (s = b = NaN, c = 0).  Attention and
- * hetis_kv4_fetch use exactly the values held.
+ * and the value held is f16(s * (16 + c) + b), rounded once; c = 0 where s = 0.  s is a product with the
+ * fp32 number nearest to 1 / 15, rounded to fp32 and then to fp16: where (hi - lo) / 15 lies half way between
+ * two fp16 numbers (or 2^-22 of itself from there) a division may give the other one.  Values are first cut
+ * to +-20480, so that b is finite; a group with a NaN holds NaN throughout (s = b = NaN, c = 0).  Attention
+ * and hetis_kv4_fetch use exactly the values held.
+ * Values that were fetched and are stored again need not come back the same: s and b are computed anew
+ * from them and may be the next fp16 number (0.2 % of the values of rows drawn from N(0, 1), 5 % from
+ * N(3, 1), off by up to 0.008).  hetis_kv4_move (hetis_evict.h) and copies of whole tiles keep the bytes.
  *
  * Tiles.  A (block, head) tile takes 10 * D bytes, the same in K and in V pools, and starts at BYTE
  *     block * kv_stride_block + head * kv_stride_head
@@ -59,7 +64,8 @@ int hetis_kv4_append(const hetis_attn_shape *shape, const void *k_new, const voi
                      void *stream);
 
 /* General store by (sequence id, position, head id), like hetis_kv_store: entries of one call may name
- * any rows, also rows of one tile (if two name the same row, which one is held is unspecified). */
+ * any rows, also rows of one tile (if two name the same row, what that row holds is unspecified: its pieces and its
+ * scales may come from either). */
 int hetis_kv4_store(const hetis_attn_shape *shape, const void *k_new, const void *v_new,
                     const int32_t *token_seq, const int32_t *token_pos, int32_t n_tokens,
                     const int32_t *block_table, const int32_t *head_ids, int32_t n_sel_heads,

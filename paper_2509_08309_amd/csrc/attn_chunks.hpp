@@ -9,9 +9,10 @@
 //                      tiles, dim n D/16 + j (A, row block j) and the probabilities of head n (B), which are
 //                      what the first product and exp2 leave in its registers.  A group has at most 8 heads:
 //                      columns n and n + 8 are the same head, the first with the probability cut to fp16, the
-//                      second with what the cut left over, so that the sums hold 21 bits of a probability
-//                      (rounded to fp16 alone, outputs were off by 2.8e-4 of them, now by 1.8e-4, which is their
-//                      own rounding; 32 long rows of 13 heads 61.3 -> 62.4 us, calls in a row).
+//                      second with what the cut left over, so that the sums miss 2^-20 of a probability at
+//                      most, or 2^-24 of the wave's largest where that is more (rounded to fp16 alone, outputs
+//                      were off by 2.8e-4 of them, now by 2.1e-4, which is their own rounding; 128 x 13 rows of
+//                      median 800 tokens 61.3 -> 62.4 us, calls in a row).
 //
 // A row (sequence, head) is cut into chunks of kCkTokens tokens, always at the same places; the four waves
 // of a workgroup take a quarter of a chunk's tile pairs each and fold their sums through LDS.  Rows of more

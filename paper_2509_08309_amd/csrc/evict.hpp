@@ -8,9 +8,11 @@
 // wanted, the lowest slots first, and numbers the holes before the new length and the kept slots behind it.
 // Counts are integers: the result is the same run to run.
 //
-// What bounds it is latency, a chain of barriers, not the 8 bytes a slot: a thread reads its slots once, all
-// at the same time, and keeps their keys in registers.  Rows longer than the registers of a workgroup hold
-// are read again in every step, window by window.
+// What bounds it is latency, not the 8 bytes a slot: a thread reads its slots all at the same time and keeps their
+// keys in registers, but up to three passes, each with its barriers, two numberings, and lists that are read back from
+// memory follow one another (64 rows of 8k to 24k slots 37 us, 23 MB read and written, vector units 8 % busy).  Weights
+// and positions are read a second time where slots move and where the output arrays are others.  Rows longer than the
+// registers of a workgroup hold are read again in every step, window by window.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -150,6 +150,9 @@ __device__ __forceinline__ int kv4_place(const P &p, int64_t b, int64_t pos, int
 }
 
 // D/8 lanes per entry, 16 bytes of K and 16 bytes of V a lane, one selected head a workgroup.
+// What bounds a store of many rows is arithmetic: 447 616 rows of 128 dims 79 us, vector units 82 % busy, 231 MB read and
+// 79 written (72 that the rows take; 98 % of the writes are whole 64-byte pieces).  A fetch of them is bound by memory:
+// 55 us, 86 MB read and 229 written.
 template <int D>
 __device__ __forceinline__ void kv4_store_row(const Kv4RowParams &p, int64_t n, int sel, int x)
 {
@@ -239,7 +242,8 @@ struct KvMoveParams {
 };
 
 // x: groups of moves, y: selected heads, z: sequences.  16 lanes a row of the fp16 cache (8 at D = 64), four of
-// the 4-bit one: its rows are small, and what a thread waits for is a chain of three loads.
+// the 4-bit one: its rows are small, and what a thread waits for is a chain of three loads (221 632 rows of 128 dims 40
+// us, 85 MB read and 44 written for 71 that the rows take, vector units 5 % busy; 237 405 fp16 rows 56 us, 4.4 TB/s).
 template <int D, bool KV4>
 constexpr int kv_move_lanes() { return KV4 ? 4 : D / 8; }
 

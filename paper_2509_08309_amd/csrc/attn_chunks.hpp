@@ -608,7 +608,9 @@ __global__ void __launch_bounds__(kCkThreads, chunk_residents(D, KV4)) chunk_ker
             for (int w = 0; w < kCkWaves; ++w)
 #pragma unroll
                 for (int e = 0; e < kFoldDims; ++e) o[e] += f[w] * lds.o[turn][w][j][d + e];
-            if constexpr (!KV4) infinite_dims<D>(p, cur, p.scores + (row * r + j) * p.slots, d, M, o);
+            if constexpr (!KV4) {
+                if (sum == sum) infinite_dims<D>(p, cur, p.scores + (row * r + j) * p.slots, d, M, o);
+            }
             // A chunk whose scores are all -inf adds nothing to its row (log-sum-exp -inf); only a row of such tokens
             // alone is NaN.
             const bool whole = cur.L <= kCkTokens;
@@ -675,7 +677,7 @@ __device__ __forceinline__ void combine_heads(const float *lp, const float *op, 
             if (c + e * G < chunks) o += v[e] * fast_exp2(w[e] - all);      // (no 0 * inf of a chunk read twice)
     }
     // (as in infinite_dims: chunks whose weight is 0 in fp32)
-    if (o[0] + o[1] + o[2] + o[3] != o[0] + o[1] + o[2] + o[3]) {
+    if (o[0] + o[1] + o[2] + o[3] != o[0] + o[1] + o[2] + o[3] && all == all) {
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
         for (int c = grp; c < chunks; c += G) {

@@ -1,7 +1,7 @@
 """MI355X-native head-subset decode Attention over a block-paged KV cache.
 
 The product is the HIP library built from csrc/ (C ABI in include/: hetis_attn.h, hetis_kv.h,
-hetis_kv4.h, hetis_evict.h);
+hetis_kv4.h, hetis_evict.h, hetis_rope.h, hetis_prefill.h, hetis_select.h);
 `binding` exposes it under the same names, `workloads` draws seeded inputs.
 Importing this package loads nothing; the library is loaded on first call and
 its absence is an error, never a fallback.
@@ -23,4 +23,8 @@ from .binding import (  # noqa: F401
     hetis_attn_decode_weights_workspace_bytes, hetis_attn_decode_weights_ws, hetis_kv4_append,
     hetis_kv4_fetch, hetis_kv4_move, hetis_kv4_store, hetis_kv4_tile_bytes, hetis_kv_evict,
     hetis_kv_move,
+    HETIS_ROPE_BASE, HETIS_ROPE_LINEAR, HETIS_ROPE_PARTS, HETIS_ROPE_PLAIN, hetis_attn_prefill,
+    hetis_attn_prefill_workspace_bytes, hetis_attn_prefill_ws, hetis_kv_append_rope, hetis_kv_bounds,
+    hetis_kv_select, hetis_kv_select_workspace_bytes, hetis_kv_select_ws, hetis_kv_store_rope, hetis_rope,
+    hetis_rope_frequencies, hetis_rope_rows, make_rope,
 )

@@ -32,6 +32,7 @@ HETIS_ERR_DEVICE_WAIT = -10
 HETIS_ATTN_CONTROL_BYTES = 256
 HETIS_ATTN_STATIC_SCRATCH_BYTES = 32 << 20
 HETIS_KV4_GROUP = 32
+HETIS_ROPE_PLAIN, HETIS_ROPE_LINEAR, HETIS_ROPE_BASE, HETIS_ROPE_PARTS = 0, 1, 2, 3
 
 
 class hetis_attn_shape(C.Structure):
@@ -45,6 +46,11 @@ class hetis_kv_pool(C.Structure):
     _fields_ = [("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("block_size", C.c_int32),
                 ("reserved", C.c_int32), ("num_blocks", C.c_int64),
                 ("kv_stride_block", C.c_int64), ("kv_stride_head", C.c_int64)]
+
+
+class hetis_rope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float),
+                ("norm_eps", C.c_float)]
 
 
 class hetis_dispatch_device(C.Structure):
@@ -181,6 +187,30 @@ def load(build_if_missing: bool = False):
     for name in ("hetis_kv_move", "hetis_kv4_move"):
         getattr(lib, name).restype = C.c_int
         getattr(lib, name).argtypes = [shp, vp, vp, i32, vp, vp, i32, i64, vp, vp, vp]
+    rope, f64 = C.POINTER(hetis_rope), C.c_double
+    lib.hetis_rope_frequencies.restype = C.c_int
+    lib.hetis_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp]
+    lib.hetis_rope_rows.restype = C.c_int
+    lib.hetis_rope_rows.argtypes = [rope, vp, vp, i64, vp, vp, i32, i32, i32, vp, i64, vp]
+    lib.hetis_kv_append_rope.restype = C.c_int
+    lib.hetis_kv_append_rope.argtypes = [shp, rope, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i64, vp, vp, vp, vp]
+    lib.hetis_kv_store_rope.restype = C.c_int
+    lib.hetis_kv_store_rope.argtypes = [shp, rope, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, i64, vp, vp,
+                                        vp, vp]
+    lib.hetis_attn_prefill.restype = C.c_int
+    lib.hetis_attn_prefill.argtypes = [shp, vp, vp, i32, vp, vp, vp, vp, vp, i32, f32, vp, vp]
+    lib.hetis_attn_prefill_ws.restype = C.c_int
+    lib.hetis_attn_prefill_ws.argtypes = [shp, vp, vp, i32, vp, vp, vp, vp, vp, i32, f32, vp, vp, C.c_size_t, vp]
+    lib.hetis_attn_prefill_workspace_bytes.restype = C.c_int
+    lib.hetis_attn_prefill_workspace_bytes.argtypes = [shp, i32, i32, C.POINTER(C.c_size_t)]
+    lib.hetis_kv_bounds.restype = C.c_int
+    lib.hetis_kv_bounds.argtypes = [shp, vp, vp, vp, vp, vp, i32, i64, vp, vp, vp]
+    lib.hetis_kv_select.restype = C.c_int
+    lib.hetis_kv_select.argtypes = [shp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
+    lib.hetis_kv_select_ws.restype = C.c_int
+    lib.hetis_kv_select_ws.argtypes = [shp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, C.c_size_t, vp]
+    lib.hetis_kv_select_workspace_bytes.restype = C.c_int
+    lib.hetis_kv_select_workspace_bytes.argtypes = [shp, i32, C.POINTER(C.c_size_t)]
     lib.call = _Calls(lib)
     _lib = lib
     return lib
@@ -195,7 +225,7 @@ class _Calls:
         native = os.path.exists(MARSHAL_PATH)
         if native:
             from . import _marshal
-            _marshal.structs(hetis_attn_shape, hetis_kv_pool)
+            _marshal.structs(hetis_attn_shape, hetis_kv_pool, hetis_rope)
         for name in ("hetis_attn_decode", "hetis_attn_decode_ws", "hetis_attn_decode_step",
                      "hetis_attn_decode_step_ws", "hetis_attn_decode_pairs", "hetis_attn_decode_pairs_ws",
                      "hetis_attn_decode_pairs_step", "hetis_attn_decode_pairs_step_ws",
@@ -204,7 +234,9 @@ class _Calls:
                      "hetis_kv_copy_tiles", "hetis_attn_decode_kv4", "hetis_attn_decode_kv4_ws",
                      "hetis_kv4_append", "hetis_kv4_store", "hetis_kv4_fetch", "hetis_attn_decode_weights",
                      "hetis_attn_decode_weights_ws", "hetis_attn_decode_kv4_weights",
-                     "hetis_attn_decode_kv4_weights_ws", "hetis_kv_evict", "hetis_kv_move", "hetis_kv4_move"):
+                     "hetis_attn_decode_kv4_weights_ws", "hetis_kv_evict", "hetis_kv_move", "hetis_kv4_move",
+                     "hetis_rope_rows", "hetis_kv_append_rope", "hetis_kv_store_rope", "hetis_attn_prefill",
+                     "hetis_attn_prefill_ws", "hetis_kv_bounds", "hetis_kv_select", "hetis_kv_select_ws"):
             fn = getattr(lib, name)
             setattr(self, name, _marshal.bind(name, C.cast(fn, C.c_void_p).value) if native else _by_ctypes(fn))
 
@@ -560,6 +592,87 @@ def hetis_kv4_move(shape, move_src, move_dst, max_moves, block_table, head_ids, 
                    num_blocks, k_cache, v_cache, stream=None) -> int:
     return (_lib or load()).call.hetis_kv4_move(shape, move_src, move_dst, max_moves, block_table,
         head_ids, n_sel_heads, num_blocks, k_cache, v_cache, _stream(stream))
+
+
+def make_rope(rot_dim, interleaved=False, magnitude=1.0, norm_eps=1e-6) -> hetis_rope:
+    return hetis_rope(rot_dim, int(interleaved), magnitude, norm_eps)
+
+
+def hetis_rope_frequencies(rot_dim, base, scaling, factor, length, low, high, inv_freq) -> int:
+    """inv_freq: float64 numpy array of rot_dim / 2 (host)."""
+    return load().hetis_rope_frequencies(int(rot_dim), float(base), int(scaling), float(factor),
+                                         float(length), float(low), float(high), _ptr(inv_freq))
+
+
+def hetis_rope_rows(rope, inv_freq, rows, stride_token, norm_weight, positions, n_tokens, n_heads,
+                    head_dim, out, out_stride_token, stream=None) -> int:
+    return (_lib or load()).call.hetis_rope_rows(rope, inv_freq, rows, stride_token, norm_weight,
+        positions, n_tokens, n_heads, head_dim, out, out_stride_token, _stream(stream))
+
+
+def hetis_kv_append_rope(shape, rope, inv_freq, q, q_weight, k_new, k_weight, v_new, block_table,
+                         seq_lens, n_seen, head_ids, n_sel_heads, num_blocks, q_out, k_cache, v_cache,
+                         stream=None) -> int:
+    return (_lib or load()).call.hetis_kv_append_rope(shape, rope, inv_freq, q, q_weight, k_new,
+        k_weight, v_new, block_table, seq_lens, n_seen, head_ids, n_sel_heads, num_blocks, q_out,
+        k_cache, v_cache, _stream(stream))
+
+
+def hetis_kv_store_rope(shape, rope, inv_freq, q, q_weight, k_new, k_weight, v_new, token_seq,
+                        token_pos, rope_pos, n_tokens, block_table, head_ids, n_sel_heads, num_blocks,
+                        q_out, k_cache, v_cache, stream=None) -> int:
+    return (_lib or load()).call.hetis_kv_store_rope(shape, rope, inv_freq, q, q_weight, k_new,
+        k_weight, v_new, token_seq, token_pos, rope_pos, n_tokens, block_table, head_ids, n_sel_heads,
+        num_blocks, q_out, k_cache, v_cache, _stream(stream))
+
+
+def hetis_attn_prefill(shape, q, q_starts, n_tokens, k_cache, v_cache, block_table, seq_lens, head_ids,
+                       n_sel_heads, scale, out, stream=None) -> int:
+    return (_lib or load()).call.hetis_attn_prefill(shape, q, q_starts, n_tokens, k_cache, v_cache,
+        block_table, seq_lens, head_ids, n_sel_heads, scale, out, _stream(stream))
+
+
+def hetis_attn_prefill_ws(shape, q, q_starts, n_tokens, k_cache, v_cache, block_table, seq_lens,
+                          head_ids, n_sel_heads, scale, out, workspace, workspace_bytes,
+                          stream=None) -> int:
+    return (_lib or load()).call.hetis_attn_prefill_ws(shape, q, q_starts, n_tokens, k_cache, v_cache,
+        block_table, seq_lens, head_ids, n_sel_heads, scale, out, workspace, workspace_bytes,
+        _stream(stream))
+
+
+def hetis_attn_prefill_workspace_bytes(shape, n_tokens, n_sel_heads):
+    """(status, bytes)."""
+    n = C.c_size_t(0)
+    rc = load().hetis_attn_prefill_workspace_bytes(C.byref(shape), int(n_tokens), int(n_sel_heads),
+                                                   C.byref(n))
+    return rc, n.value
+
+
+def hetis_kv_bounds(shape, k_cache, block_table, seq_lens, first_pos, head_ids, n_sel_heads, num_blocks,
+                    codes, scales, stream=None) -> int:
+    return (_lib or load()).call.hetis_kv_bounds(shape, k_cache, block_table, seq_lens, first_pos,
+        head_ids, n_sel_heads, num_blocks, codes, scales, _stream(stream))
+
+
+def hetis_kv_select(shape, q, codes, scales, block_table, seq_lens, head_ids, n_sel_heads, n_pages,
+                    n_sink, n_recent, tiles, sel_lens, stream=None) -> int:
+    return (_lib or load()).call.hetis_kv_select(shape, q, codes, scales, block_table, seq_lens,
+        head_ids, n_sel_heads, n_pages, n_sink, n_recent, tiles, sel_lens, _stream(stream))
+
+
+def hetis_kv_select_ws(shape, q, codes, scales, block_table, seq_lens, head_ids, n_sel_heads, n_pages,
+                       n_sink, n_recent, tiles, sel_lens, workspace, workspace_bytes,
+                       stream=None) -> int:
+    return (_lib or load()).call.hetis_kv_select_ws(shape, q, codes, scales, block_table, seq_lens,
+        head_ids, n_sel_heads, n_pages, n_sink, n_recent, tiles, sel_lens, workspace, workspace_bytes,
+        _stream(stream))
+
+
+def hetis_kv_select_workspace_bytes(shape, n_sel_heads):
+    """(status, bytes)."""
+    n = C.c_size_t(0)
+    rc = load().hetis_kv_select_workspace_bytes(C.byref(shape), int(n_sel_heads), C.byref(n))
+    return rc, n.value
 
 
 def hetis_profiler_fit(h, g, tau, n, abc, accuracy=None) -> int:

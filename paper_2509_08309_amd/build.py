@@ -11,8 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhetis_attn.so")
 # (the name carries the interpreter's version: another one does not pick up what it cannot load)
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = ["hetis_attn.hip", "hetis_chunks.hip", "hetis_evict.hip", "hetis_kv.hip", "hetis_kv4.hip", "hetis_profiler.hip",
-           "hetis_dispatch.hip"]
+SOURCES = ["hetis_attn.hip", "hetis_chunks.hip", "hetis_evict.hip", "hetis_kv.hip", "hetis_kv4.hip", "hetis_rope.hip",
+           "hetis_prefill.hip", "hetis_select.hip", "hetis_profiler.hip", "hetis_dispatch.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
@@ -26,7 +26,8 @@ def sources():
     for root, _, files in os.walk(CSRC):
         out += [os.path.join(root, f) for f in files if f.endswith((".hip", ".hpp", ".h", ".cpp"))]
     inc = os.path.join(os.path.dirname(HERE), "include")
-    out += [os.path.join(inc, f) for f in ("hetis_attn.h", "hetis_kv.h", "hetis_kv4.h", "hetis_evict.h", "hetis_profiler.h",
+    out += [os.path.join(inc, f) for f in ("hetis_attn.h", "hetis_kv.h", "hetis_kv4.h", "hetis_evict.h", "hetis_rope.h",
+                                         "hetis_prefill.h", "hetis_select.h", "hetis_profiler.h",
                                          "hetis_dispatch.h")]
     return out
 

@@ -2,10 +2,11 @@
 // C ABI's, without a Python function or a ctypes conversion for each.  A launch costs the runtime 2.9 us on the
 // host; conversions in Python and ctypes added 2.1 us to a decode call's and 2.0 to an append's, now 0.6 and
 // 0.5.  Launches that the GPU has done sooner wait for the host: appends 6.1 us a pass -> 4.8.
-//   structs(shape, pool): the ctypes classes of hetis_attn_shape and hetis_kv_pool, before the first call.
+//   structs(shape, pool, rope): the ctypes classes of hetis_attn_shape, hetis_kv_pool and hetis_rope, before the
+//     first call.
 //   bind(name, address) -> callable for the library function `name` at `address`; None for other names.
 // The callable takes positional arguments only, as many as the C function.  By the type of the parameter:
-// structs are instances of those classes (a pool may be None), pointers are None, an int, or
+// structs are instances of those classes (a pool or a rope may be None), pointers are None, an int, or
 // an object with data_ptr() (a torch tensor) or .ctypes.data (a numpy array); numbers are converted as int()
 // and float() do.  The interpreter lock is released during the call, as ctypes does.
 #define PY_SSIZE_T_CLEAN
@@ -21,11 +22,14 @@
 #include "../../include/hetis_evict.h"
 #include "../../include/hetis_kv.h"
 #include "../../include/hetis_kv4.h"
+#include "../../include/hetis_prefill.h"
+#include "../../include/hetis_rope.h"
+#include "../../include/hetis_select.h"
 
 namespace {
 
 PyObject *s_data_ptr, *s_ctypes, *s_data;      // interned attribute names
-PyObject *shape_type, *pool_type;               // the binding's classes of the two structures
+PyObject *shape_type, *pool_type, *rope_type;   // the binding's classes of the structures
 
 bool address_of(PyObject *o, void **out)
 {
@@ -73,12 +77,13 @@ bool convert(PyObject *o, T &out)
         return true;
     } else {
         using S = std::remove_cv_t<std::remove_pointer_t<T>>;
-        if constexpr (std::is_same_v<S, hetis_attn_shape> || std::is_same_v<S, hetis_kv_pool>) {
-            if (o == Py_None && std::is_same_v<S, hetis_kv_pool>) {      // (a shape has to be one)
+        constexpr bool is_shape = std::is_same_v<S, hetis_attn_shape>, is_pool = std::is_same_v<S, hetis_kv_pool>;
+        if constexpr (is_shape || is_pool || std::is_same_v<S, hetis_rope>) {
+            if (o == Py_None && !is_shape) {                             // (a shape has to be one)
                 out = nullptr;
                 return true;
             }
-            PyObject *type = std::is_same_v<S, hetis_kv_pool> ? pool_type : shape_type;
+            PyObject *type = is_shape ? shape_type : is_pool ? pool_type : rope_type;
             const int is = type ? PyObject_IsInstance(o, type) : 0;
             if (is <= 0) {
                 if (is == 0) PyErr_Format(PyExc_TypeError, "a structure argument is a %s", Py_TYPE(o)->tp_name);
@@ -137,7 +142,9 @@ PyMethodDef calls[] = {
     HETIS_CALL(hetis_kv4_store), HETIS_CALL(hetis_kv4_fetch), HETIS_CALL(hetis_attn_decode_weights),
     HETIS_CALL(hetis_attn_decode_weights_ws), HETIS_CALL(hetis_attn_decode_kv4_weights),
     HETIS_CALL(hetis_attn_decode_kv4_weights_ws), HETIS_CALL(hetis_kv_evict), HETIS_CALL(hetis_kv_move),
-    HETIS_CALL(hetis_kv4_move),
+    HETIS_CALL(hetis_kv4_move), HETIS_CALL(hetis_rope_rows), HETIS_CALL(hetis_kv_append_rope),
+    HETIS_CALL(hetis_kv_store_rope), HETIS_CALL(hetis_attn_prefill), HETIS_CALL(hetis_attn_prefill_ws),
+    HETIS_CALL(hetis_kv_bounds), HETIS_CALL(hetis_kv_select), HETIS_CALL(hetis_kv_select_ws),
 };
 
 PyObject *bind(PyObject *, PyObject *args)
@@ -158,12 +165,14 @@ PyObject *bind(PyObject *, PyObject *args)
 
 PyObject *structs(PyObject *, PyObject *args)
 {
-    PyObject *shape, *pool;
-    if (!PyArg_ParseTuple(args, "OO", &shape, &pool)) return nullptr;
+    PyObject *shape, *pool, *rope;
+    if (!PyArg_ParseTuple(args, "OOO", &shape, &pool, &rope)) return nullptr;
     Py_INCREF(shape);
     Py_INCREF(pool);
+    Py_INCREF(rope);
     Py_XSETREF(shape_type, shape);
     Py_XSETREF(pool_type, pool);
+    Py_XSETREF(rope_type, rope);
     Py_RETURN_NONE;
 }
 
@@ -180,6 +189,6 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_ctypes = PyUnicode_InternFromString("ctypes");
     s_data = PyUnicode_InternFromString("data");
     if (!s_data_ptr || !s_ctypes || !s_data) return nullptr;
-    shape_type = pool_type = nullptr;
+    shape_type = pool_type = rope_type = nullptr;
     return PyModule_Create(&module);
 }

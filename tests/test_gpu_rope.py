@@ -1,0 +1,266 @@
+"""Rotary positions on the GPU against the definition in 64 bits: rows, and queries, keys and values on the way into
+the cache."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2509_08309_amd as H
+from paper_2509_08309_amd import workloads as W
+from prefill_reference import frequencies, rotate
+
+from gpu_harness import SENTINEL, bits
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def i32(a):
+    return torch.from_numpy(np.ascontiguousarray(np.asarray(a, dtype=np.int32))).to(DEV)
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def sentinel(*shape):
+    out = torch.empty(shape, dtype=torch.float16, device=DEV)
+    out.view(torch.int16).fill_(np.int16(SENTINEL))
+    return out
+
+
+def close(got, ref, tol, where=""):
+    bad = ~(np.abs(got.astype(np.float64) - ref) <= tol)
+    assert not bad.any(), (where, np.argwhere(bad)[:3].tolist(), np.abs(got.astype(np.float64) - ref).max())
+
+
+POSITIONS = [0, 1, 2, 7, 100, 4095, 131071, 1 << 20, 2 ** 31 - 1, -1, -5000, -2 ** 31]
+
+
+@pytest.mark.parametrize("D,rot", [(64, 64), (64, 16), (64, 48), (128, 128), (128, 64), (128, 16), (128, 112)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("n,heads", [(1, 1), (12, 9), (37, 33)])
+def test_rows(D, rot, interleaved, norm, n, heads):
+    rng = np.random.default_rng(D + rot + n)
+    x = rng.standard_normal((n, heads, D)).astype(np.float16)
+    pos = np.resize(np.array(POSITIONS), n)
+    w = (1 + 0.3 * rng.standard_normal(D)).astype(np.float16) if norm else None
+    f = frequencies(rot)
+    out = sentinel(n, heads, D)
+    rope = H.make_rope(rot, interleaved, 1.25, 1e-5)
+    H.check(H.hetis_rope_rows(rope, dev(f), dev(x), 0, None if w is None else dev(w), i32(pos), n, heads, D, out, 0))
+    torch.cuda.synchronize()
+    ref, tol = rotate(x, pos, f, interleaved, w, 1e-5, 1.25)
+    close(out.cpu().numpy(), ref, tol)
+
+
+@pytest.mark.parametrize("n,heads,extra", [(5, 6, 8), (3000, 40, 24), (700, 8, 1032)])
+def test_strides_and_in_place(n, heads, extra):
+    """Query rows of a fused buffer, rotated into rows of their own and in place: the same bits, and what lies between
+    the rows stays."""
+    D, f = 128, frequencies(64)
+    rng = np.random.default_rng(n)
+    fused = rng.standard_normal((n, heads * D + extra)).astype(np.float16)
+    pos, rope = i32(rng.integers(0, 5000, n)), H.make_rope(64)
+    a, freq = dev(fused), dev(f)
+    apart = sentinel(n, heads * D + 40)
+    H.check(H.hetis_rope_rows(rope, freq, a, heads * D + extra, None, pos, n, heads, D, apart, heads * D + 40))
+    torch.cuda.synchronize()
+    assert np.array_equal(bits(a), fused.view(np.uint16)) and (bits(apart)[:, heads * D:] == SENTINEL).all()
+    ref, tol = rotate(fused[:, :heads * D].reshape(n, heads, D), pos.cpu().numpy(), f)
+    close(apart.cpu().numpy()[:, :heads * D].reshape(n, heads, D), ref, tol)
+    H.check(H.hetis_rope_rows(rope, freq, a, heads * D + extra, None, pos, n, heads, D, a, heads * D + extra))
+    torch.cuda.synchronize()
+    assert np.array_equal(bits(a)[:, :heads * D], bits(apart)[:, :heads * D])
+    assert np.array_equal(bits(a)[:, heads * D:], fused.view(np.uint16)[:, heads * D:])
+
+
+def test_position_zero_and_no_rotation():
+    """Position 0 keeps the bits of the rotated dims, and the others are kept at any position."""
+    x = np.random.default_rng(1).standard_normal((40, 3, 64)).astype(np.float16)
+    out = sentinel(40, 3, 64)
+    pos = np.zeros(40)
+    pos[20:] = 77
+    H.check(H.hetis_rope_rows(H.make_rope(32), dev(frequencies(32)), dev(x), 0, None, i32(pos), 40, 3, 64, out, 0))
+    torch.cuda.synchronize()
+    got, x = bits(out), x.view(np.uint16)
+    assert np.array_equal(got[:20], x[:20]) and np.array_equal(got[..., 32:], x[..., 32:])
+
+
+def test_values_that_are_not_finite():
+    """They stay in their pair without a norm, and in their row with one; rows of zeros with eps = 0 are NaN."""
+    x = np.ones((4, 2, 64), dtype=np.float16)
+    x[0, 0, 3], x[1, 1, 40], x[2, 0] = np.inf, np.nan, 0
+    f, pos = dev(frequencies(64)), i32([9, 9, 9, 9])
+    for w in (None, dev(np.ones(64, dtype=np.float16))):
+        out = sentinel(4, 2, 64)
+        H.check(H.hetis_rope_rows(H.make_rope(64, norm_eps=0.0), f, dev(x), 0, w, pos, 4, 2, 64, out, 0))
+        torch.cuda.synchronize()
+        fin = np.isfinite(out.cpu().numpy().astype(np.float32))
+        if w is None:
+            bad = np.argwhere(~fin).tolist()
+            assert bad == [[0, 0, 3], [0, 0, 35], [1, 1, 8], [1, 1, 40]]
+        else:
+            assert not fin[1, 1].any() and not fin[2, 0].any() and fin[3].all() and fin[0, 1].all() and not fin[0, 0, [3, 35]].any()
+
+
+# ------------------------------------------------------------------ into the cache
+
+class Cache:
+    def __init__(self, lens, hq, hkv, D, seed, n, max_blocks=None):
+        self.lens, self.hq, self.hkv, self.D = np.asarray(lens), hq, hkv, D
+        self.rng = rng = np.random.default_rng(seed)
+        self.mb = max_blocks or max(1, -(-int(max(lens)) // 16))
+        self.table, self.nb = W.build_block_table(self.lens.astype(np.int32), self.mb, 16, rng, extra_blocks=1)
+        self.q = rng.standard_normal((n, hq, D)).astype(np.float16)
+        self.k, self.v = (rng.standard_normal((n, hkv, D)).astype(np.float16) for _ in range(2))
+        self.weights = [(1 + 0.3 * rng.standard_normal(D)).astype(np.float16) for _ in range(2)]
+
+    def shape(self, **kw):
+        return H.make_shape(len(self.lens), self.hq, self.hkv, self.D, self.mb, **kw)
+
+    def expect(self, heads, seq, slot, pos, f, interleaved, norm, q_out, pools, skipped=()):
+        """Everything as the definition has it: rotated rows to tolerance, values bit for bit, the rest untouched."""
+        r = self.hq // self.hkv
+        wq, wk = self.weights if norm else (None, None)
+        named = [h for h in range(self.hq) if h // r in heads]
+        live = [n for n in range(len(seq)) if n not in skipped]
+        if q_out is not None:
+            ref, tol = rotate(self.q, pos, f, interleaved, wq, 1e-6, 1.0)
+            got = q_out.cpu().numpy()
+            close(got[live][:, named], ref[live][:, named], tol[live][:, named], "q")
+            rest = np.ones(got.shape[:2], dtype=bool)
+            rest[np.ix_(live, named)] = False
+            assert (bits(q_out)[rest] == SENTINEL).all()
+        ref, tol = rotate(self.k, pos, f, interleaved, wk, 1e-6, 1.0)
+        kp, vp = (p.cpu().numpy() for p in pools)
+        untouched = np.ones(kp.shape[:3], dtype=bool)
+        for n in live:
+            blk = self.table[seq[n], slot[n] // 16]
+            for g in heads:
+                close(kp[blk, g, slot[n] % 16], ref[n, g], tol[n, g], ("k", n, g))
+                assert np.array_equal(vp[blk, g, slot[n] % 16].view(np.uint16), self.v[n, g].view(np.uint16))
+                untouched[blk, g, slot[n] % 16] = False
+        for p in (kp, vp):
+            assert (p.view(np.uint16)[untouched] == SENTINEL).all()
+
+
+@pytest.mark.parametrize("hq,hkv,D,heads", [(8, 8, 64, [1, 6]), (16, 2, 128, [1]), (6, 2, 128, [0, 1]), (40, 40, 128, list(range(13)))])
+@pytest.mark.parametrize("interleaved,norm,seen,with_q", [(False, False, False, True), (True, True, True, True), (False, True, True, False)])
+def test_append(hq, hkv, D, heads, interleaved, norm, seen, with_q):
+    lens = np.array([1, 16, 17, 0, 100, 33, 64])
+    c = Cache(lens, hq, hkv, D, 5, len(lens))
+    f = frequencies(D)
+    n_seen = lens + c.rng.integers(0, 900, len(lens)) if seen else None
+    pools = [sentinel(c.nb, hkv, 16, D) for _ in range(2)]
+    q_out = sentinel(*c.q.shape) if with_q else None
+    wq, wk = (dev(w) for w in c.weights) if norm else (None, None)
+    H.check(H.hetis_kv_append_rope(c.shape(), H.make_rope(D, interleaved), dev(f), dev(c.q) if with_q else None, wq, dev(c.k),
+                                   wk, dev(c.v), i32(c.table), i32(lens), None if n_seen is None else i32(n_seen), i32(heads),
+                                   len(heads), c.nb, q_out, *pools))
+    torch.cuda.synchronize()
+    c.expect(heads, np.arange(len(lens)), lens - 1, (n_seen if seen else lens) - 1, f, interleaved, norm, q_out, pools, skipped=[3])
+
+
+@pytest.mark.parametrize("hq,hkv,D,rot,heads", [(4, 4, 64, 32, [0, 2, 3]), (16, 2, 128, 128, [1, 0]), (24, 8, 128, 96, [7])])
+@pytest.mark.parametrize("positions", [False, True])
+def test_store(hq, hkv, D, rot, heads, positions):
+    lens = np.array([200, 0, 31, 90, 1])
+    seq = np.repeat(np.arange(5), lens)
+    slot = np.concatenate([np.arange(n) for n in lens])
+    order = np.random.default_rng(2).permutation(len(seq))
+    seq, slot = seq[order], slot[order]
+    c = Cache(lens, hq, hkv, D, 6, len(seq))
+    pos = slot + c.rng.integers(0, 100, len(seq)) if positions else slot
+    f = frequencies(rot)
+    pools, q_out = [sentinel(c.nb, hkv, 16, D) for _ in range(2)], sentinel(*c.q.shape)
+    H.check(H.hetis_kv_store_rope(c.shape(), H.make_rope(rot, True), dev(f), dev(c.q), None, dev(c.k), None, dev(c.v), i32(seq),
+                                  i32(slot), i32(pos) if positions else None, len(seq), i32(c.table), i32(heads), len(heads),
+                                  c.nb, q_out, *pools))
+    torch.cuda.synchronize()
+    c.expect(heads, seq, slot, pos, f, True, False, q_out, pools)
+    # without a rotation to speak of it is hetis_kv_store
+    plain = [sentinel(c.nb, hkv, 16, D) for _ in range(2)]
+    turned = [sentinel(c.nb, hkv, 16, D) for _ in range(2)]
+    H.check(H.hetis_kv_store(c.shape(), dev(c.k), dev(c.v), i32(seq), i32(slot), len(seq), i32(c.table), i32(heads), len(heads), c.nb, *plain))
+    H.check(H.hetis_kv_store_rope(c.shape(), H.make_rope(rot), dev(0 * f), None, None, dev(c.k), None, dev(c.v), i32(seq), i32(slot),
+                                  None, len(seq), i32(c.table), i32(heads), len(heads), c.nb, None, *turned))
+    torch.cuda.synchronize()
+    for a, b in zip(plain, turned):
+        assert np.array_equal(bits(a), bits(b))
+
+
+def test_entries_that_point_outside_are_skipped():
+    c = Cache([40, 40, 40], 4, 2, 64, 7, 9)
+    seq = np.array([0, -1, 3, 1, 1, 2, 2, 0, 1])
+    slot = np.array([5, 5, 5, -1, 48, 20, 39, 33, 7])
+    c.table[2, 1] = c.nb                                   # slot 20 of sequence 2
+    c.table[0, 2] = -1                                     # slot 33 of sequence 0
+    heads = [1]
+    pools, q_out = [sentinel(c.nb, 2, 16, 64) for _ in range(2)], sentinel(*c.q.shape)
+    f = frequencies(64)
+    H.check(H.hetis_kv_store_rope(c.shape(), H.make_rope(64), dev(f), dev(c.q), None, dev(c.k), None, dev(c.v), i32(seq), i32(slot),
+                                  None, 9, i32(c.table), i32([1, 5, -1]), 1, c.nb, q_out, *pools))
+    torch.cuda.synchronize()
+    c.expect(heads, seq, slot, slot, f, False, False, q_out, pools, skipped=[1, 2, 3, 4, 5, 7])
+    before = [bits(p) for p in pools] + [bits(q_out)]
+    H.check(H.hetis_kv_store_rope(c.shape(), H.make_rope(64), dev(f), dev(c.q), None, dev(c.k), None, dev(c.v), i32(seq), i32(slot),
+                                  None, 9, i32(c.table), i32([2, -1]), 2, c.nb, q_out, *pools))
+    torch.cuda.synchronize()
+    assert all(np.array_equal(a, bits(p)) for a, p in zip(before, pools + [q_out]))
+
+
+@pytest.mark.parametrize("n", [3, 4000])
+def test_in_place_and_heads_named_twice(n):
+    """Queries rotated in place are rotated once, however often a head is named; a subset has the bits of all heads."""
+    lens = np.full(1, n)
+    c = Cache(lens, 16, 4, 128, 8, n)
+    f, seq, slot = dev(frequencies(128)), i32(np.zeros(n)), i32(np.arange(n))
+    outs = []
+    for heads in ([0, 1, 2, 3], [2, 0, 2, 2]):
+        for in_place in (False, True):
+            q = dev(c.q)
+            q_out = q if in_place else sentinel(*c.q.shape)
+            pools = [sentinel(c.nb, 4, 16, 128) for _ in range(2)]
+            H.check(H.hetis_kv_store_rope(c.shape(), H.make_rope(128), f, q, None, dev(c.k), None, dev(c.v), seq, slot, None, n,
+                                          i32(c.table), i32(heads), len(heads), c.nb, q_out, *pools))
+            torch.cuda.synchronize()
+            outs.append([bits(q_out)] + [bits(p) for p in pools])
+    for rows in (slice(0, 4), slice(8, 12)):
+        for o in outs[1:]:
+            assert np.array_equal(o[0][:, rows], outs[0][0][:, rows])
+    assert np.array_equal(outs[3][0][:, 4:8], c.q.view(np.uint16)[:, 4:8])
+    for o in outs[2:]:
+        for a, b in zip(o[1:], outs[0][1:]):
+            assert np.array_equal(a[:, [0, 2]], b[:, [0, 2]]) and (a[:, [1, 3]] == SENTINEL).all()
+
+
+def test_a_graph_of_a_step():
+    """Append with rotation and decode, captured once, replayed with other tokens."""
+    lens = np.array([40, 100, 7])
+    c = Cache(lens, 8, 2, 64, 9, 3)
+    f, rope, bt, sl, hid = dev(frequencies(64)), H.make_rope(64), i32(c.table), i32(lens), i32([0, 1])
+    rng = np.random.default_rng(3)
+    base = [dev(rng.standard_normal((c.nb, 2, 16, 64)).astype(np.float16)) for _ in range(2)]
+
+    def step(q, k, v, q_out, pools, out):
+        H.check(H.hetis_kv_append_rope(c.shape(), rope, f, q, None, k, None, v, bt, sl, None, hid, 2, c.nb, q_out, *pools))
+        H.check(H.hetis_attn_decode(c.shape(), q_out, *pools, bt, sl, hid, 2, 0.125, out))
+
+    q, k, v = dev(c.q), dev(c.k), dev(c.v)
+    q_out, out, pools = torch.zeros_like(q), torch.zeros_like(q), [x.clone() for x in base]
+    step(q, k, v, q_out, pools, out)                       # (the library's workspace is there before the capture)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(q, k, v, q_out, pools, out)
+    for turn in range(4):
+        for t in (q, k, v):
+            t.copy_(torch.from_numpy(rng.standard_normal(tuple(t.shape)).astype(np.float16)))
+        q2, o2, p2 = torch.zeros_like(q), torch.zeros_like(q), [x.clone() for x in pools]
+        step(q, k, v, q2, p2, o2)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip([q2, o2] + p2, [q_out, out] + pools):
+            assert np.array_equal(bits(a), bits(b)), turn

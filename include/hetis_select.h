@@ -8,12 +8,13 @@
  *
  * Bounds.  Of a (block, KV head) with n rows in use, hi_d and lo_d = the largest and the smallest of its key
  * values in dim d, a = the largest of all |hi_d| and |lo_d|, in fp32:
- *     s = a / 127     codes  min(ceil(hi_d / s), 127)  and  max(floor(lo_d / s), -127)     (all 0 where s = 0)
+ *     s = a * f32(1 / 127)     codes  min(ceil(hi_d / s), 127)  and  max(floor(lo_d / s), -127)     (all 0 where s = 0)
  *     codes   int8 [num_blocks, Hkv, 2, D]: upper, then lower ones        scales  fp32 [num_blocks, Hkv]: s
- * A page with an infinite value or NaN has s = +inf and codes of 0.
+ * (s is a product with the fp32 number nearest to 1 / 127, rounded to fp32; a division may give its neighbour.)  A page
+ * with an infinite value or NaN has s = +inf and codes of 0.
  *
- * Score.  Of a query head j of the group, in fp32: t_j = max_d |q_jd| / 127, c_jd = rint(q_jd / t_j) (ties to
- * even; 0 where t_j = 0), and for a page
+ * Score.  Of a query head j of the group, in fp32: t_j = max_d |q_jd| * f32(1 / 127), c_jd = rint(q_jd / t_j)
+ * (ties to even; 0 where t_j = 0), and for a page
  *     score = max_j (f32(sum_d c_jd * (c_jd > 0 ? upper_d : lower_d)) * t_j) * s
  * The sum is in whole numbers, so that the score, and with it the choice, has one value whatever the order.  A
  * page of scale +inf scores +inf; a query head with an infinite value or NaN takes no part (a group of such

@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(BoundsParams p)
         most = max(most, dpp_u32<0x141>(most));
         if (D == 128) most = max(most, dpp_u32<0x140>(most));
         const bool finite = most < 0x7c00u;
-        const float s = finite ? (float)__builtin_bit_cast(_Float16, (unsigned short)most) / 127.f : INFINITY;
+        const float s = finite ? (float)__builtin_bit_cast(_Float16, (unsigned short)most) * (1.f / 127.f) : INFINITY;
         // lanes 4 LR: upper and lower codes of four dims each
         const int part = lane / LR, lower = part & 1, at = part >> 1;
         if (part < 4) {
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(SelectParams p)
         o = lanes_xor<32>(most);
         most = max(o.x, o.y);
         counts = counts && most < 0x7c00u;
-        t = (float)__builtin_bit_cast(_Float16, (unsigned short)most) / 127.f;
+        t = (float)__builtin_bit_cast(_Float16, (unsigned short)most) * (1.f / 127.f);
 #pragma unroll
         for (int w = 0; w < DIMS / 4; ++w) {                       // four codes a word
             unsigned up = 0, down = 0;

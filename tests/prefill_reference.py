@@ -85,7 +85,7 @@ def bounds(keys):
     if not np.isfinite(x).all():
         return np.zeros((2, x.shape[1]), dtype=np.int64), np.float32(np.inf)
     hi, lo = x.max(0), x.min(0)
-    s = np.float32(max(np.abs(hi).max(), np.abs(lo).max()) / np.float32(127))
+    s = np.float32(max(np.abs(hi).max(), np.abs(lo).max())) * (np.float32(1) / np.float32(127))
     if s == 0:
         return np.zeros((2, x.shape[1]), dtype=np.int64), s
     return np.stack([np.minimum(np.ceil(hi / s), 127), np.maximum(np.floor(lo / s), -127)]).astype(np.int64), s
@@ -97,7 +97,7 @@ def scores(q, codes, scales):
     for row in q.astype(np.float32):
         if not np.isfinite(row).all():
             continue
-        t = np.float32(np.abs(row).max() / np.float32(127))
+        t = np.abs(row).max() * (np.float32(1) / np.float32(127))
         c = np.rint(row / t).astype(np.int64) if t > 0 else np.zeros(len(row), dtype=np.int64)
         whole = np.where(c > 0, c * codes[:, 0], c * codes[:, 1]).sum(1)
         best = np.maximum(best, whole.astype(np.float32) * t)

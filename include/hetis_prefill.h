@@ -20,8 +20,8 @@
  * sequence's cache up to its position, on n_b and on L_b only: a head-subset call returns the matching rows of the
  * all-heads call bit for bit, and results are the same run to run.
  *
- * Supported: head_dim in {64, 128}; block_size 16; r in {1, 2, 4, 8}; batch <= 65535, n_kv_heads <= 1024,
- * max_blocks_per_seq <= 2^24.  Pools, queries and outputs start at 16-byte boundaries.
+ * Supported: head_dim in {64, 128}; block_size 16; r in {1, 2, 4, 8}; batch <= 32768, n_kv_heads <= 1024,
+ * max_blocks_per_seq <= 2^24, n_tokens * r * n_sel_heads < 2^37.  Pools, queries and outputs start at 16-byte boundaries.
  */
 #ifndef HETIS_PREFILL_H
 #define HETIS_PREFILL_H
@@ -35,7 +35,7 @@ extern "C" {
 /*
  *   shape        host
  *   q            fp16 [n_tokens, Hq, D]
- *   q_starts     int32 [B + 1], ascending, from 0
+ *   q_starts     int32 [B + 1], ascending; rows ahead of q_starts[0] are left untouched as well
  *   n_tokens     host, rows of q and out, >= 0 (0 is a no-op)
  *   k_cache, v_cache, block_table, seq_lens, head_ids, n_sel_heads, scale   as for hetis_attn_decode
  *   out          fp16 [n_tokens, Hq, D], not q

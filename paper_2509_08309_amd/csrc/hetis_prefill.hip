@@ -18,8 +18,39 @@ static int check_prefill_shape(const hetis_attn_shape *s, int32_t n_tokens, int3
     if (rc == HETIS_OK) rc = check_grid(s);
     if (rc != HETIS_OK) return rc;
     if (n_tokens < 0) return HETIS_ERR_BAD_SHAPE;
+    if (s->batch > (int)kArrivalSlots / kPfSplitTiles) return HETIS_ERR_UNSUPPORTED;
     const int r = s->n_q_heads / s->n_kv_heads;
     return r == 1 || r == 2 || r == 4 || r == 8 ? HETIS_OK : HETIS_ERR_UNSUPPORTED;
+}
+
+// Control words and arrival counters of the other calls stay as they are; behind them partial results of sequences that
+// are cut along the cache.
+struct PrefillLayout {
+    size_t partial = 0, total = HETIS_ATTN_CONTROL_BYTES;
+    int64_t rows = 0;                       // of a head
+    bool by_sequence = false;
+};
+
+static PrefillLayout prefill_layout(const hetis_attn_shape *s, int32_t n_tokens, int32_t n_sel)
+{
+    PrefillLayout w;
+    const int64_t steps = ((int64_t)s->max_blocks_per_seq * kBlockTokens + kPfStep - 1) / kPfStep;
+    const int64_t segs = std::min<int64_t>((steps + kPfOneTileSteps - 1) / kPfOneTileSteps, kPfSplitItems);
+    if (segs <= 1 || n_tokens == 0) return w;            // no row of the table is long enough
+    // a row in every segment, or the items that a sequence can have: whichever is less
+    const int64_t by_row = segs * n_tokens * (s->n_q_heads / s->n_kv_heads);
+    const int64_t by_sequence = (int64_t)s->batch * kPfSplitItems * kPfRows;
+    w.by_sequence = by_sequence < by_row;
+    w.rows = std::min(by_row, by_sequence);
+    w.partial = HETIS_ATTN_CONTROL_BYTES + kArrivalBytes;
+    w.total = align256(w.partial + (size_t)n_sel * w.rows * (s->head_dim + 2) * sizeof(float));
+    return w;
+}
+
+// Heads of a launch: those whose tiles have arrival counters.
+static int heads_of_a_launch(const hetis_attn_shape *s, int32_t n_sel)
+{
+    return (int)std::min<int64_t>(n_sel, kArrivalSlots / kPfSplitTiles / s->batch);
 }
 
 static int prefill_call(const hetis_attn_shape *shape, const void *q, const int32_t *q_starts, int32_t n_tokens,
@@ -31,11 +62,13 @@ static int prefill_call(const hetis_attn_shape *shape, const void *q, const int3
     int rc = check_prefill_shape(shape, n_tokens, n_sel, &c);
     if (rc != HETIS_OK) return rc;
     if (!q || !q_starts || !k || !v || !block_table || !seq_lens || !head_ids || !out) return HETIS_ERR_NULL;
-    const size_t need = HETIS_ATTN_CONTROL_BYTES;
+    const PrefillLayout lay = prefill_layout(shape, n_tokens, n_sel);
     const hipStream_t st = (hipStream_t)stream;
-    rc = owned ? owned_workspace(need, st, true, &workspace) : check_workspace(workspace, workspace_bytes, need);
+    if (owned && n_tokens == 0) return HETIS_OK;
+    rc = owned ? owned_workspace(lay.total, st, true, &workspace) : check_workspace(workspace, workspace_bytes, lay.total);
     if (rc != HETIS_OK) return rc;
     if (n_tokens == 0) return HETIS_OK;
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
     PrefillParams p{};
     p.q = (const __half *)q;
     p.k = (const __half *)k;
@@ -55,14 +88,37 @@ static int prefill_call(const hetis_attn_shape *shape, const void *q, const int3
     p.group_shift = r == 8 ? 3 : r / 2;
     p.max_blocks_per_seq = shape->max_blocks_per_seq;
     p.tiles = n_tokens / (kPfRows / r) + shape->batch;
+    if ((int64_t)p.tiles * n_sel > 1 << 30) return HETIS_ERR_UNSUPPORTED;
     p.scale_log2 = std::max(std::fabs(scale) * kLog2e, FLT_MIN);         // (0 times a masked score would be NaN)
     p.q_sign = std::signbit(scale) ? 0x80008000u : 0u;
-    const int64_t items = (int64_t)n_sel * p.tiles;
-    if (items > 1 << 23) return HETIS_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)items);
-    if (shape->head_dim == 128) prefill_kernel<128><<<grid, kPfThreads, 0, st>>>(p);
-    else prefill_kernel<64><<<grid, kPfThreads, 0, st>>>(p);
-    return launched();
+    p.partial = reinterpret_cast<float *>(ws + lay.partial);
+    p.control = reinterpret_cast<unsigned int *>(ws);
+    p.arrivals = reinterpret_cast<unsigned int *>(ws + HETIS_ATTN_CONTROL_BYTES);
+    p.partial_rows = lay.rows;
+    p.rows_by_sequence = lay.by_sequence;
+    const int cus = device_cu_count();
+    if (cus <= 0) return HETIS_ERR_LAUNCH;
+    const int heads = heads_of_a_launch(shape, n_sel);
+    for (int h = 0; h < n_sel; h += heads) {
+        p.head_ids = head_ids + h;
+        p.n_sel = std::min(heads, n_sel - h);
+        // two workgroups a compute unit, and no more than there can be items; whole rounds of the queues
+        const int64_t items = ((int64_t)p.tiles + (lay.rows ? (int64_t)shape->batch * kPfSplitItems : 0)) * p.n_sel;
+        if (lay.rows == 0 && items <= 2 * cus) {
+            if (shape->head_dim == 128) prefill_direct_kernel<128><<<(unsigned)items, kPfThreads, 0, st>>>(p);
+            else prefill_direct_kernel<64><<<(unsigned)items, kPfThreads, 0, st>>>(p);
+            rc = launched();
+            if (rc != HETIS_OK) return rc;
+            continue;
+        }
+        const int64_t grid = std::min<int64_t>(items, 2 * cus);
+        const dim3 places((unsigned)((grid + kPfQueues - 1) / kPfQueues * kPfQueues));
+        if (shape->head_dim == 128) prefill_kernel<128><<<places, kPfThreads, 0, st>>>(p);
+        else prefill_kernel<64><<<places, kPfThreads, 0, st>>>(p);
+        rc = launched();
+        if (rc != HETIS_OK) return rc;
+    }
+    return HETIS_OK;
 }
 
 }  // namespace hetis
@@ -95,7 +151,7 @@ int hetis_attn_prefill_workspace_bytes(const hetis_attn_shape *shape, int32_t n_
     CacheStrides c;
     const int rc = check_prefill_shape(shape, n_tokens, n_sel_heads, &c);
     if (rc != HETIS_OK) return rc;
-    *bytes = HETIS_ATTN_CONTROL_BYTES;
+    *bytes = prefill_layout(shape, n_tokens, n_sel_heads).total;
     return HETIS_OK;
 }
 

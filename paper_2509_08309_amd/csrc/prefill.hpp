@@ -19,6 +19,8 @@
 #include <limits.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "attn_common.hpp"
 
 namespace hetis {
@@ -34,8 +36,12 @@ struct PrefillParams {
     const __half *k, *v;
     const int32_t *q_starts, *block_table, *seq_lens, *head_ids;
     __half *out;                            // [n_tokens, Hq, D]
+    float *partial;                         // [n_sel, partial_rows] rows of D, then [n_sel, partial_rows] pairs
+    unsigned int *control, *arrivals;       // arrivals: [batch, n_sel, kPfSplitTiles]
     int64_t stride_block, stride_head;      // elements
+    int64_t partial_rows;                   // of a head
     int32_t n_tokens, batch, n_sel, n_q_heads, group_shift, max_blocks_per_seq, tiles;
+    int32_t rows_by_sequence;               // partial rows are numbered by sequence and item, otherwise by segment and row
     float scale_log2;                       // the scale's magnitude
     uint32_t q_sign;                        // its sign, for the two query values of a word
 };
@@ -44,23 +50,49 @@ constexpr int kPfWaves = 4;
 constexpr int kPfThreads = 64 * kPfWaves;
 constexpr int kPfRows = 32 * kPfWaves;      // rows of a tile
 constexpr int kPfStep = 64;                 // cached tokens of a step
+// A sequence of few tiles over a long cache is cut along the cache as well, by its own numbers only: into at most
+// kPfSplitItems / tiles segments of at least kPfOneTileSteps or kPfFewTilesSteps steps.
+constexpr int kPfSplitTiles = 8, kPfSplitItems = 32, kPfOneTileSteps = 8, kPfFewTilesSteps = 16;
+constexpr int kPfQueues = 8;
+enum : int { kPfCtlTickets = 16, kPfCtlGone = 24 };      // control words: a queue's tickets, workgroups finished
 
-// A tile's number is q_starts[b] / tokens + b + its number in its sequence b (tokens: of a tile): at least as many
-// numbers as a sequence has tiles lie between its first and the next one's.  The sequence of a number by its
-// lanes: 64 starts at a time.
-__device__ __forceinline__ int prefill_sequence(const PrefillParams &p, int tile, int token_shift, int lane)
+// What there is to do for a sequence.
+struct PrefillSequence {
+    int start, fresh, len, rows, tiles, segs, seg_steps;    // rows: tokens with a row; seg_steps: steps of a segment
+    __device__ __forceinline__ int items() const { return tiles * segs; }
+};
+__device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillParams &p, int start, int end, int len)
 {
-    int lo = 0, n = p.batch;                // the answer is in [lo, lo + n)
-    while (n > 1) {
-        const int step = (n + 63) / 64;
-        const int b = lo + lane * step;
-        const bool ok = lane * step < n && (max(p.q_starts[min(b, p.batch)], 0) >> token_shift) + b <= tile;
-        const int found = max(__popcll(__ballot(ok)) - 1, 0);
-        lo += found * step;
-        n = min(step, n - found * step);
+    PrefillSequence s;
+    s.start = start;
+    s.fresh = end - start;
+    s.len = len;
+    // (rows that q does not have are no work)
+    s.rows = s.start < 0 || s.start >= p.n_tokens ? 0 : min(max(s.fresh, 0), p.n_tokens - s.start);
+    const int steps = (min(max(s.len, 0), p.max_blocks_per_seq * kBlockTokens) + kPfStep - 1) / kPfStep;
+    s.tiles = (int)((((int64_t)s.rows << p.group_shift) + kPfRows - 1) / kPfRows);
+    s.segs = 1;
+    s.seg_steps = max(steps, 1);
+    if (s.tiles >= 1 && s.tiles <= kPfSplitTiles) {
+        const int least = s.tiles == 1 ? kPfOneTileSteps : kPfFewTilesSteps;
+        const int want = min((steps + least - 1) / least, kPfSplitItems / s.tiles);
+        if (want > 1) {
+            s.seg_steps = (steps + want - 1) / want;
+            s.segs = (steps + s.seg_steps - 1) / s.seg_steps;
+        }
     }
-    return lo;
+    return s;
 }
+
+__device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillParams &p, int b)
+{
+    return prefill_sequence(p, p.q_starts[b], p.q_starts[b + 1], p.seq_lens[b]);
+}
+
+struct PrefillItem {
+    int b, head, tile, seg;                 // head: place in head_ids
+    PrefillSequence seq;
+};
 
 // All bits of the halves that are infinite or NaN.
 __device__ __forceinline__ unsigned not_finite(unsigned x)
@@ -74,34 +106,151 @@ typedef __attribute__((address_space(3))) const unsigned char *LdsByte;
 typedef __attribute__((address_space(3))) pf_i16x4 *LdsI16x4;
 typedef __attribute__((address_space(3))) const pf_f16x8 *LdsF16x8;
 
+// Descriptor of the first `nbytes` bytes of a tile, like tile_rsrc.
+__device__ __forceinline__ i32x4 tile_descriptor(const __half *tile, int nbytes)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(tile);
+    return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)a), __builtin_amdgcn_readfirstlane((int)(a >> 32)),
+                 __builtin_amdgcn_readfirstlane(nbytes), 0x00020000};
+}
+
+// A page into LDS at `to`, past the registers: load e's sixteen bytes of lane i go to `to` + (64 e + i) 16.  (By hand,
+// because the compiler waits for such loads ahead of any later LDS read; the caller waits, once a step.  There are no
+// registers that wait for them.  The wait states are those that a load needs behind a vector instruction that has
+// written its descriptor, and behind a change of M0.)
 template <int D>
-__global__ void __launch_bounds__(kPfThreads, 2) prefill_kernel(PrefillParams p)
+__device__ __forceinline__ void page_to_lds(i32x4 r, int from0, int from1, int from2, int from3, unsigned to)
+{
+    if constexpr (D == 128)
+        asm volatile("s_mov_b32 m0, %5\n\ts_nop 4\n\t"
+                     "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
+                     "buffer_load_dwordx4 %1, %4, 0 offen offset:1024 lds\n\t"
+                     "buffer_load_dwordx4 %2, %4, 0 offen offset:2048 lds\n\t"
+                     "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds"
+                     :: "v"(from0), "v"(from1), "v"(from2), "v"(from3), "s"(r), "s"(to) : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %3\n\ts_nop 4\n\t"
+                     "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
+                     "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds"
+                     :: "v"(from0), "v"(from3), "s"(r), "s"(to) : "memory");
+}
+
+// Pieces of a row change places with its number, so that the lanes that read together meet different banks: 16 rows at
+// the same piece (K), four rows at four neighbouring pieces (V).
+template <int D>
+__device__ __forceinline__ int k_piece(int r, int c) { return c ^ (D == 128 ? r & 15 : r >> 1 & 7); }
+template <int D>
+__device__ __forceinline__ int v_piece(int r, int c) { return c ^ (D == 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2); }
+
+template <int D>
+struct PrefillLds {
+    unsigned char kv[2][2][kPfStep * D * 2];            // K, V; two steps
+    int odd_from[3][D], any_odd;                        // first token with a value of +inf, -inf, NaN that some rows do not see
+    int before[kPfThreads + 1];                         // items of a queue ahead of a thread's sequences
+    int order[kPfThreads], key[kPfThreads];             // sequences by their place, and what they are placed by
+    int starts[kPfThreads + 1], lens[kPfThreads];
+    int sums[kPfWaves], totals[kPfWaves][kPfQueues];
+    int item[2], ticket, last;
+};
+
+template <int D>
+__device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<D> &sh, const PrefillItem &item)
 {
     constexpr int KS = D / 16;              // products of a score
     constexpr int DB = D / 32;              // row blocks of O^T
     constexpr int CH = D / 8;               // 16-byte pieces of a row
     constexpr int PER = D / 32;             // pieces of a page in a lane
-    __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][kPfStep * D * 2];
-    __shared__ int odd_from[3][D], any_odd; // first token with a value of +inf, -inf, NaN that some rows do not see
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));           // (what follows from it stays in here: kept over all items it was spilled)
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, h = lane >> 5;
-    const int g = p.head_ids[blockIdx.x % p.n_sel];
-    const int token_shift = 7 - p.group_shift;          // tokens of a tile: 128 / r
-    const int tile = p.tiles - 1 - (int)(blockIdx.x / p.n_sel);
-    const int b = __builtin_amdgcn_readfirstlane(prefill_sequence(p, tile, token_shift, lane));
-    const int start = p.q_starts[b], fresh = p.q_starts[b + 1] - start, L = p.seq_lens[b];
-    const int t_first = (tile - (max(start, 0) >> token_shift) - b) << token_shift;
-    if (t_first < 0 || t_first >= fresh) return;
-    const int t_last = min(t_first + (1 << token_shift), fresh) - 1;
+    // (scalar loads: a vector load would wait for what is on its way to LDS)
+    typedef const __attribute__((address_space(4))) int32_t *Scalars;
+    const int b = item.b, g = reinterpret_cast<Scalars>(reinterpret_cast<uintptr_t>(p.head_ids))[item.head];
+    const PrefillSequence &seq = item.seq;
+    const int start = seq.start, fresh = seq.fresh, L = seq.len;
+    const int t_first = item.tile << (7 - p.group_shift);               // tokens of a tile: 128 / r
+    if (t_first >= seq.rows) return;
+    const int t_last = min(t_first + (kPfRows >> p.group_shift), seq.rows) - 1;
     const int seen = min(max(L - fresh + t_last + 1, 0), p.max_blocks_per_seq * kBlockTokens);
-    const int steps = (seen + kPfStep - 1) / kPfStep, pages = (seen + kBlockTokens - 1) / kBlockTokens;
+    const int pages = (seen + kBlockTokens - 1) / kBlockTokens;
+    const int all_steps = (seen + kPfStep - 1) / kPfStep;
+    const int first = item.seg * seq.seg_steps, steps = min(all_steps, first + seq.seg_steps);
+    if (item.seg > 0 && first >= all_steps) return;
+    const int tile_segs = max((all_steps + seq.seg_steps - 1) / seq.seg_steps, 1);
 
     // this lane's row
     const int row = wave * 32 + n, token = t_first + (row >> p.group_shift);
     const int64_t at = (int64_t)start + token;
-    const bool there = token <= t_last && at >= 0 && at < p.n_tokens;
+    const bool there = token <= t_last;
     const int pos = L - fresh + token;                  // sees tokens up to it
     const int64_t element = (at * p.n_q_heads + ((int64_t)g << p.group_shift) + (row & ((1 << p.group_shift) - 1))) * D;
+    // the wave's rows: how many there are, position of the first, steps up to the last one's position
+    const int wave_rows = min(max(((t_last + 1 - t_first) << p.group_shift) - wave * 32, 0), 32);
+    const int pos_lo = L - fresh + t_first + ((wave * 32) >> p.group_shift);
+    const int pos_hi = L - fresh + t_first + ((wave * 32 + wave_rows - 1) >> p.group_shift);
+    const int own_steps = wave_rows > 0 ? min(steps, (max(pos_hi + 1, 0) + kPfStep - 1) / kPfStep) : first;
+
+    const auto table = reinterpret_cast<Scalars>(reinterpret_cast<uintptr_t>(p.block_table + (int64_t)b * p.max_blocks_per_seq));
+    const int64_t head = (int64_t)g * p.stride_head;
+    // Wave w brings page w of a step, straight into LDS: lane i's sixteen bytes of load e land at (64 e + i) 16 of the
+    // page's place, so that it is the lane that asks for the piece that belongs there.  Pages behind the last one, and
+    // rows behind the last token, arrive as zeros.
+    int from_k[PER];
+    const int from_v = lane / CH * (2 * D) + v_piece<D>(lane / CH, lane % CH) * 16;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) from_k[e] = lane / CH * (2 * D) + k_piece<D>(e * (64 / CH) + lane / CH, lane % CH) * 16;
+    auto bring = [&](int step, bool values) {
+        const int page = step * (kPfStep / kBlockTokens) + wave;
+        const int rows = min(max(seen - page * kBlockTokens, 0), kBlockTokens);
+        const int64_t block = table[min(page, pages - 1)];
+        const i32x4 r = tile_descriptor((values ? p.v : p.k) + block * p.stride_block + head, rows * D * 2);
+        const unsigned to = (unsigned)(uintptr_t)(LdsByte)&sh.kv[values][step & 1][wave * (kBlockTokens * D * 2)];
+        if (values) page_to_lds<D>(r, from_v, from_v, from_v, from_v, to);
+        else page_to_lds<D>(r, from_k[0], from_k[1], from_k[PER - 2], from_k[PER - 1], to);
+    };
+    // Tokens that some of the rows do not see may hold values that are not finite, and 0 times such a value is not 0:
+    // these go into the products as 0, and are added at the end to the rows that see them.
+    const int seen_by_all = L - fresh + t_first;        // the last token that every row of the tile sees
+    auto clean = [&](int step) {
+        if ((step + 1) * kPfStep - 1 <= seen_by_all) return;
+        u32x4 *own = reinterpret_cast<u32x4 *>(&sh.kv[1][step & 1][wave * (kBlockTokens * D * 2)]);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const u32x4 x = own[e * 64 + lane];
+            if (not_finite(x[0]) | not_finite(x[1]) | not_finite(x[2]) | not_finite(x[3])) {
+                const int r = e * (64 / CH) + lane / CH, t = step * kPfStep + wave * kBlockTokens + r, d = v_piece<D>(r, lane % CH) * 8;
+                unsigned short *half = reinterpret_cast<unsigned short *>(&own[e * 64 + lane]);
+#pragma clang loop unroll(disable)
+                for (int f = 0; f < 8; ++f) {
+                    if ((half[f] & 0x7c00u) != 0x7c00u) continue;
+                    atomicMin(&sh.odd_from[odd_kind(half[f])][d + f], t);
+                    half[f] = 0;
+                }
+                sh.any_odd = 1;
+            }
+        }
+    };
+
+    pf_f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float mc = kNegBig, l = 0.f;                        // reference of the weights (times c), sum of the weights
+    const float c = p.scale_log2;
+
+    for (int i = tid; i < 3 * D; i += kPfThreads) sh.odd_from[0][i] = INT_MAX;
+    if (tid == 0) sh.any_odd = 0;
+    // where this lane reads its rows of K and (by the sixteen lanes that transpose) its dims of V
+    const int k_at = n * (2 * D) + k_piece<D>(n, h) * 16;
+    int v_at[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        const int r = 4 * h + (lane >> 2 & 3), cc = lane & 3;
+        v_at[d] = r * (2 * D) + v_piece<D>(r, 4 * d + 2 * (lane >> 4 & 1) + (cc >> 1)) * 16 + (cc & 1) * 8;
+    }
+    if (first < steps) bring(first, false);
     pf_f16x8 q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -111,162 +260,224 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_kernel(PrefillParams p)
         for (int e = 0; e < 4; ++e) x[e] ^= p.q_sign;
         q[s] = __builtin_bit_cast(pf_f16x8, x);
     }
-    // positions of the wave's rows, first and last
-    const int pos_lo = L - fresh + t_first + ((wave * 32) >> p.group_shift);
-    const int pos_hi = min(L - fresh + t_last, L - fresh + t_first + ((wave * 32 + 31) >> p.group_shift));
-
-    const int32_t *table = p.block_table + (int64_t)b * p.max_blocks_per_seq;
-    const int64_t head = (int64_t)g * p.stride_head;
-    u32x4 kv[2][PER];
-    // wave w brings page w of a step; pages behind the last one, and rows behind the last token, are zeros
-    auto load = [&](int step) {
-        const int page = step * (kPfStep / kBlockTokens) + wave;
-        const int rows = min(max(seen - page * kBlockTokens, 0), kBlockTokens);
-        const int64_t block = table[min(page, pages - 1)];
-        const __amdgpu_buffer_rsrc_t rk = tile_rsrc(p.k + block * p.stride_block + head, rows * D * 2);
-        const __amdgpu_buffer_rsrc_t rv = tile_rsrc(p.v + block * p.stride_block + head, rows * D * 2);
-#pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            kv[0][e] = __builtin_amdgcn_raw_buffer_load_b128(rk, (e * 64 + lane) * 16, 0, 0);
-            kv[1][e] = __builtin_amdgcn_raw_buffer_load_b128(rv, (e * 64 + lane) * 16, 0, 0);
-        }
+    pf_f32x16 s[2];
+    // the piece of K that a lane needs for product e of 32 tokens' scores (half of a step)
+    auto key = [&](int step, int half, int e) {
+        return *(LdsF16x8)((LdsByte)&sh.kv[0][step & 1][0] + (k_at ^ (32 * e)) + half * 32 * (2 * D));
     };
-    // Pieces of a row change places with its number, so that the lanes that read together meet different banks: 16
-    // rows at the same piece (K), four rows at four neighbouring pieces (V).
-    auto k_piece = [](int r, int c) { return c ^ (D == 128 ? r & 15 : r >> 1 & 7); };
-    auto v_piece = [](int r, int c) { return c ^ (D == 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2); };
-    const int seen_by_all = L - fresh + t_first;        // the last token that every row of the tile sees
-    auto store = [&](int step) {
-        const int buffer = step & 1;
-        // Tokens that some of the rows do not see may hold values that are not finite, and 0 times such a value is not 0:
-        // these go into the products as 0, and are added at the end to the rows that see them.
-        if ((step + 1) * kPfStep - 1 > seen_by_all) {
+    auto clear = [&](int half) {
 #pragma unroll
-            for (int e = 0; e < PER; ++e)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const unsigned bad = not_finite(kv[1][e][w]);
-                    if (bad) {
-                        const int i = e * 64 + lane, t = step * kPfStep + wave * kBlockTokens + i / CH, d = i % CH * 8 + 2 * w;
-                        if (bad & 0xffffu) atomicMin(&odd_from[odd_kind(kv[1][e][w])][d], t);
-                        if (bad & 0xffff0000u) atomicMin(&odd_from[odd_kind(kv[1][e][w] >> 16)][d + 1], t);
-                        any_odd = 1;
-                        kv[1][e][w] &= ~bad;
-                    }
-                }
-        }
-#pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            const int i = e * 64 + lane, r = wave * kBlockTokens + i / CH, c = i % CH;
-            *reinterpret_cast<u32x4 *>(&lds[buffer][0][r * (2 * D) + k_piece(r, c) * 16]) = kv[0][e];
-            *reinterpret_cast<u32x4 *>(&lds[buffer][1][r * (2 * D) + v_piece(r, c) * 16]) = kv[1][e];
-        }
+        for (int e = 0; e < 16; ++e) s[half][e] = 0.f;
     };
-
-    pf_f32x16 o[DB];
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-    float m = kNegBig, l = 0.f;
-    const float c = p.scale_log2;
-
-    for (int i = tid; i < 3 * D; i += kPfThreads) odd_from[0][i] = INT_MAX;
-    if (tid == 0) any_odd = 0;
-    // where this lane reads its rows of K and (by the sixteen lanes that transpose) its dims of V
-    const int k_at = n * (2 * D) + k_piece(n, h) * 16;
-    int v_at[DB];
-#pragma unroll
-    for (int d = 0; d < DB; ++d) {
-        const int r = 4 * h + (lane >> 2 & 3), cc = lane & 3;
-        v_at[d] = r * (2 * D) + v_piece(r, 4 * d + 2 * (lane >> 4 & 1) + (cc >> 1)) * 16 + (cc & 1) * 8;
-    }
-    __syncthreads();
-    if (steps > 0) {
-        load(0);
-        store(0);
-        __syncthreads();
-    }
-    for (int step = 0; step < steps; ++step) {
-        if (step + 1 < steps) load(step + 1);
+    auto score = [&](int half, int e, pf_f16x8 k) { s[half] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[e], s[half], 0, 0, 0); };
+    // Brings the reference up to date: a weight is at most 2^8, and as long as that holds the reference stays (a row's
+    // own scores decide, whatever its neighbours need).
+    auto settle = [&](int step) {
         const int t0 = step * kPfStep;
-        if (t0 <= pos_hi) {
-            const LdsByte ks = (LdsByte)&lds[step & 1][0][0], vs = (LdsByte)&lds[step & 1][1][0];
-            pf_f32x16 s[2];
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[tb][e] = 0.f;
-#pragma unroll
-                for (int e = 0; e < KS; ++e) {
-                    const pf_f16x8 a = *(LdsF16x8)(ks + (k_at ^ (32 * e)) + tb * 32 * (2 * D));
-                    s[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[e], s[tb], 0, 0, 0);
-                }
-            }
-            const bool border = t0 + kPfStep - 1 > pos_lo;
-            if (border) {
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (t0 + tb * 32 + e / 4 * 8 + 4 * h + e % 4 > pos) s[tb][e] = -INFINITY;
-            }
-            float top = -INFINITY;
+        if (t0 + kPfStep - 1 > pos_lo) {
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) top = fmaxf(top, s[tb][e]);
-            top = max_xor32(top);
-            if (__builtin_amdgcn_ballot_w64(top > m) != 0) {
-                const float m_new = fmaxf(m, top), alpha = fast_exp2((m - m_new) * c);
-                m = m_new;
-                l *= alpha;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[d] *= alpha;
-            }
-            const float mc = m * c;
-            pf_f16x8 pr[4];
-            float sum = 0.f;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float w = fast_exp2(__builtin_fmaf(s[t / 2][8 * (t % 2) + e], c, -mc));
-                    sum += w;
-                    pr[t][e] = (_Float16)w;
-                }
-            l += sum;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    // V^T of 16 tokens, 32 dims
-                    pf_i16x4 x[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsI16x4)(vs + v_at[d] + (16 * t + 8 * e) * (2 * D)));
-                    const pf_f16x4 lo = __builtin_bit_cast(pf_f16x4, x[0]), hi = __builtin_bit_cast(pf_f16x4, x[1]);
-                    const pf_f16x8 f = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, pr[t], o[d], 0, 0, 0);
-                }
+                for (int e = 0; e < 16; ++e)
+                    if (t0 + tb * 32 + e / 4 * 8 + 4 * h + e % 4 > pos) s[tb][e] = -INFINITY;
         }
-        if (step + 1 < steps) store(step + 1);
-        __syncthreads();
+        float top = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
+        top = max_xor32(top) * c;
+        if (__builtin_amdgcn_ballot_w64(top > mc + 8.f) != 0) {
+            const float to = top > mc + 8.f ? top : mc, alpha = fast_exp2(mc - to);
+            mc = to;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d] *= alpha;
+        }
+    };
+    const pf_f16x2 ones = {(_Float16)1.f, (_Float16)1.f};
+    pf_f16x8 pr[4];
+    // weights 2 i and 2 i + 1 of a half
+    auto weight = [&](int half, int i) {
+        pf_f16x2 w;
+#pragma unroll
+        for (int f = 0; f < 2; ++f) w[f] = (_Float16)fast_exp2(__builtin_fmaf(s[half][2 * i + f], c, -mc));
+        l = __builtin_amdgcn_fdot2(w, ones, l, false);
+        pr[2 * half + i / 4][i % 4 * 2] = w[0];
+        pr[2 * half + i / 4][i % 4 * 2 + 1] = w[1];
+    };
+    // V^T of 16 tokens, 32 dims: product i = 16 tokens t, row block d
+    auto value = [&](int step, int i) {
+        const int t = i / DB, d = i % DB;
+        const LdsByte vs = (LdsByte)&sh.kv[1][step & 1][0];
+        pf_i16x4 x[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsI16x4)(vs + v_at[d] + (16 * t + 8 * e) * (2 * D)));
+        const pf_f16x4 lo = __builtin_bit_cast(pf_f16x4, x[0]), hi = __builtin_bit_cast(pf_f16x4, x[1]);
+        return pf_f16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    // A step's weights and values, and between them the scores of the next step, each half as soon as the registers of
+    // this step's scores are free.  The order is the one written here: left to itself the compiler reads an operand just
+    // ahead of its product, or all of them and spills.
+    auto attend = [&](int step, auto with_next) {
+        constexpr bool NEXT = decltype(with_next)::value;
+        constexpr int AHEAD = 6;                        // values on their way to their products
+        pf_f16x8 k[KS], v[4 * DB];
+        if constexpr (NEXT) {
+#pragma unroll
+            for (int e = 0; e < KS; ++e) k[e] = key(step + 1, 0, e);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) weight(0, i);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (NEXT) {
+            clear(0);
+#pragma unroll
+            for (int e = 0; e < KS; ++e) {
+                score(0, e, k[e]);
+                k[e] = key(step + 1, 1, e);
+#pragma unroll
+                for (int i = 0; i < 8 / KS; ++i) weight(1, e * (8 / KS) + i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            clear(1);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) weight(1, i);
+        }
+#pragma unroll
+        for (int e = 0; e < (NEXT ? KS : 0) || e < AHEAD; ++e) {
+            if (NEXT && e < KS) score(1, e, k[e]);
+            if (e < AHEAD) v[e] = value(step, e);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4 * DB; ++i) {
+            o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[i], pr[i / DB], o[i % DB], 0, 0, 0);
+            if (i + AHEAD < 4 * DB) v[i + AHEAD] = value(step, i + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto drain = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+    auto meet = [] { asm volatile("s_barrier" ::: "memory"); };
+
+    // Step i: scores of step i + 1 beside the weights of step i, then the values of step i.  K is a step ahead of V.
+    if (first < steps) {
+        drain();
+        meet();
+        bring(first, true);
+        if (first + 1 < steps) bring(first + 1, false);
+        if (first < own_steps) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                clear(half);
+#pragma unroll
+                for (int e = 0; e < KS; ++e) score(half, e, key(first, half, e));
+            }
+        }
     }
+    auto turn = [&](int step) {
+        drain();
+        clean(step);
+        drain();
+        meet();
+        if (step + 1 < steps) bring(step + 1, true);
+        if (step + 2 < steps) bring(step + 2, false);
+    };
+    int step = first;
+    for (; step < own_steps - 1; ++step) {
+        settle(step);
+        turn(step);
+        attend(step, std::true_type());
+    }
+    if (step < own_steps) {
+        settle(step);
+        turn(step);
+        attend(step, std::false_type());
+        ++step;
+    }
+    for (; step < steps; ++step) turn(step);            // (the other waves' rows lie further on)
+    drain();
+    meet();
 
     l = sum_xor32(l);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (any_odd) {
+    if (sh.any_odd) {
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int dim = 32 * d + 8 * (e / 4) + 4 * h + e % 4;
-                if (pos >= odd_from[0][dim]) o[d][e] += INFINITY;
-                if (pos >= odd_from[1][dim]) o[d][e] -= INFINITY;
-                if (pos >= odd_from[2][dim]) o[d][e] = NAN;
+                if (pos >= sh.odd_from[0][dim]) o[d][e] += INFINITY;
+                if (pos >= sh.odd_from[1][dim]) o[d][e] -= INFINITY;
+                if (pos >= sh.odd_from[2][dim]) o[d][e] = NAN;
             }
     }
+    if (tile_segs > 1) {
+        // Partial results: of a wave's rows, four dims of each after the other, then reference and sum.  The workgroup
+        // that stores a tile's last ones adds all of them up in the order of the segments.
+        const int64_t local = p.rows_by_sequence ? 0 : (int64_t)item.tile * kPfRows + wave * 32;
+        auto place = [&](int seg) {
+            return (int64_t)item.head * p.partial_rows +
+                   (p.rows_by_sequence ? (int64_t)b * (kPfSplitItems * kPfRows) + (item.tile * seq.segs + seg) * kPfRows + wave * 32
+                                       : ((int64_t)seg * p.n_tokens << p.group_shift) + ((int64_t)start << p.group_shift) + local);
+        };
+        const int64_t pairs = (int64_t)p.n_sel * p.partial_rows * D;
+        auto rows_at = [&](int seg) { return coherent_rsrc(p.partial + place(seg) * D, wave_rows * D * 4); };
+        auto pairs_at = [&](int seg) { return p.partial + pairs + (place(seg) + n) * 2; };
+        if (n < wave_rows) {
+            const __amdgpu_buffer_rsrc_t r = rows_at(item.seg);
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const f32x4 x = {o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+                    coherent_store_b128(r, ((2 * (4 * d + j) + h) * wave_rows + n) * 16, __builtin_bit_cast(u32x4, x));
+                }
+            if (h == 0) {
+                coherent_store(pairs_at(item.seg), mc);
+                coherent_store(pairs_at(item.seg) + 1, l);
+            }
+        }
+        drain();
+        meet();
+        if (tid == 0) {
+            unsigned int *count = p.arrivals + ((int64_t)b * p.n_sel + item.head) * kPfSplitTiles + item.tile;
+            sh.last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)tile_segs - 1;
+            if (sh.last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        drain();
+        meet();
+        if (!sh.last) return;
+        if (n < wave_rows) {
+            mc = kNegBig;
+            l = 0.f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+            for (int seg = 0; seg < tile_segs; ++seg) {
+                const float m2 = coherent_load(pairs_at(seg)), l2 = coherent_load(pairs_at(seg) + 1);
+                const __amdgpu_buffer_rsrc_t r = rows_at(seg);
+                const float to = fmaxf(mc, m2), was = fast_exp2(mc - to), is = fast_exp2(m2 - to);
+                mc = to;
+                l = __builtin_fmaf(l2, is, l * was);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    u32x4 x[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = coherent_load_b128(r, ((2 * (4 * d + j) + h) * wave_rows + n) * 16, 0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4 y = __builtin_bit_cast(f32x4, x[j]);
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) o[d][4 * j + f] = __builtin_fmaf(y[f], is, o[d][4 * j + f] * was);
+                    }
+                }
+            }
+        }
+    }
+
+    const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -289,6 +500,214 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_kernel(PrefillParams p)
             }
             if (there) *reinterpret_cast<u32x4 *>(p.out + element + 32 * d + 8 * (j + h)) = x;
         }
+}
+
+// The sequences, longest items first, and their items in kPfQueues queues: (sequence, head) number i belongs to queue i
+// mod 8, and workgroup w takes from queue w mod 8 as long as there is something in it, then from the others.  Workgroups
+// are handed to the chip's eight dies in turn, so the tiles that share a head's cache run on one die and meet in its L2.
+template <int D>
+struct PrefillQueues {
+    const PrefillParams &p;
+    PrefillLds<D> &sh;
+    int per, mine;                          // sequences a thread looks after; items a head of its first one
+
+    __device__ __forceinline__ int pairs_in(int queue, int rank, int *first_head) const
+    {
+        const int h0 = (queue - rank * p.n_sel) & (kPfQueues - 1);
+        *first_head = h0;
+        return h0 < p.n_sel ? (p.n_sel - 1 - h0) / kPfQueues + 1 : 0;
+    }
+    __device__ __forceinline__ PrefillSequence sequence(int b) const
+    {
+        return per == 1 ? prefill_sequence(p, sh.starts[b], sh.starts[b + 1], sh.lens[b]) : prefill_sequence(p, b);
+    }
+
+    __device__ __forceinline__ PrefillQueues(const PrefillParams &p_, PrefillLds<D> &sh_) : p(p_), sh(sh_)
+    {
+        const int tid = threadIdx.x;
+        per = (p.batch + kPfThreads - 1) / kPfThreads;
+        mine = 0;
+        if (per == 1) {
+            // by the steps of an item, descending (few sequences: each thread compares with all)
+            if (tid < p.batch) {
+                sh.starts[tid] = p.q_starts[tid];
+                sh.lens[tid] = p.seq_lens[tid];
+                if (tid == p.batch - 1) sh.starts[p.batch] = p.q_starts[p.batch];
+            }
+            __syncthreads();
+            const int key = tid < p.batch ? sequence(tid).seg_steps : -1;
+            sh.key[tid] = key;
+            __syncthreads();
+            int rank = 0;
+            for (int j = 0; j < p.batch; ++j) rank += sh.key[j] > key || (sh.key[j] == key && j < tid);
+            if (tid < p.batch) sh.order[rank] = tid;
+            __syncthreads();
+            if (tid < p.batch) mine = sequence(sh.order[tid]).items();
+        }
+        // items of every queue
+        int total[kPfQueues] = {};
+        each([&](int rank, int items) {
+            int h0;
+#pragma unroll
+            for (int y = 0; y < kPfQueues; ++y) total[y] += items * pairs_in(y, rank, &h0);
+        });
+#pragma unroll
+        for (int o = 32; o; o >>= 1)
+#pragma unroll
+            for (int y = 0; y < kPfQueues; ++y) total[y] += __shfl_xor(total[y], o);
+#pragma unroll
+        for (int y = 0; y < kPfQueues; ++y)
+            if (tid % 64 == y) sh.totals[tid / 64][y] = total[y];
+        __syncthreads();
+    }
+    // f(rank, items of a head) for this thread's sequences
+    template <class F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        if (per == 1) {
+            if ((int)threadIdx.x < p.batch) f((int)threadIdx.x, mine);
+            return;
+        }
+        for (int i = 0, rank = threadIdx.x * per; i < per && rank < p.batch; ++i, ++rank) f(rank, prefill_sequence(p, rank).items());
+    }
+    __device__ __forceinline__ int total(int queue) const
+    {
+        int t = 0;
+#pragma unroll
+        for (int w = 0; w < kPfWaves; ++w) t += sh.totals[w][queue];
+        return t;
+    }
+    // items of the queue ahead of each thread's
+    __device__ __forceinline__ void open(int queue)
+    {
+        const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+        int sum = 0, h0;
+        each([&](int rank, int items) { sum += items * pairs_in(queue, rank, &h0); });
+        int upto = sum;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(upto, o);
+            upto += lane >= o ? x : 0;
+        }
+        if (lane == 63) sh.sums[wave] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kPfWaves; ++w) upto += w < wave ? sh.sums[w] : 0;
+        sh.before[tid + 1] = upto;
+        if (tid == 0) sh.before[0] = 0;
+        __syncthreads();
+    }
+    // Item k of the open queue: of a sequence the tiles that see most first, one for each head.
+    __device__ __forceinline__ PrefillItem find(int queue, int k)
+    {
+        const int tid = threadIdx.x;
+        if (sh.before[tid] <= k && k < sh.before[tid + 1]) {
+            int rem = k - sh.before[tid], h0;
+            for (int rank = tid * per; rank < p.batch; ++rank) {
+                const int items = (per == 1 ? mine : prefill_sequence(p, rank).items()) * pairs_in(queue, rank, &h0);
+                if (rem < items) {
+                    sh.item[0] = rank;
+                    sh.item[1] = rem;
+                    break;
+                }
+                rem -= items;
+            }
+        }
+        __syncthreads();
+        const int rank = __builtin_amdgcn_readfirstlane(sh.item[0]), rem = __builtin_amdgcn_readfirstlane(sh.item[1]);
+        PrefillItem item;
+        item.b = per == 1 ? __builtin_amdgcn_readfirstlane(sh.order[rank]) : rank;
+        if (per == 1)
+            item.seq = prefill_sequence(p, __builtin_amdgcn_readfirstlane(sh.starts[item.b]),
+                                        __builtin_amdgcn_readfirstlane(sh.starts[item.b + 1]), __builtin_amdgcn_readfirstlane(sh.lens[item.b]));
+        else
+            item.seq = prefill_sequence(p, item.b);
+        int h0;
+        const int pairs = pairs_in(queue, rank, &h0), u = rem / pairs;
+        item.head = h0 + kPfQueues * (rem % pairs);
+        item.tile = item.seq.tiles - 1 - u / item.seq.segs;
+        item.seg = u % item.seq.segs;
+        return item;
+    }
+};
+
+// A launch of few items, none of them cut along the cache: item i is workgroup i's, and nothing is handed out.  Tile
+// numbers are q_starts[b] / tokens + b + the tile's place in its sequence b (tokens: of a tile), which leaves at least as
+// many numbers to a sequence as it has tiles; the sequence of a number is found 64 starts at a time.
+__device__ __forceinline__ PrefillItem prefill_direct(const PrefillParams &p, int number)
+{
+    const int lane = threadIdx.x % 64, token_shift = 7 - p.group_shift, tile = p.tiles - 1 - number / p.n_sel;
+    int lo = 0, n = p.batch;                // the answer is in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 63) / 64;
+        const int b = lo + lane * step;
+        const bool ok = lane * step < n && (max(p.q_starts[min(b, p.batch)], 0) >> token_shift) + b <= tile;
+        const int found = max((int)__popcll(__ballot(ok)) - 1, 0);          // (a count is unsigned)
+        lo += found * step;
+        n = min(step, n - found * step);
+    }
+    PrefillItem item;
+    item.b = __builtin_amdgcn_readfirstlane(lo);
+    item.head = number % p.n_sel;
+    item.seq = prefill_sequence(p, item.b);
+    item.tile = tile - (max(item.seq.start, 0) >> token_shift) - item.b;
+    item.seg = 0;
+    return item;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kPfThreads, 2) prefill_direct_kernel(PrefillParams p)
+{
+    __shared__ __attribute__((aligned(16))) PrefillLds<D> sh;
+    const PrefillItem item = prefill_direct(p, blockIdx.x);
+    if (item.tile >= 0) prefill_item<D>(p, sh, item);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kPfThreads, 2) prefill_kernel(PrefillParams p)
+{
+    __shared__ __attribute__((aligned(16))) PrefillLds<D> sh;
+    PrefillQueues<D> queues(p, sh);
+    const int tid = threadIdx.x, places = gridDim.x / kPfQueues;        // workgroups of a queue
+    int queue = blockIdx.x % kPfQueues, k = blockIdx.x / kPfQueues, tried = 0;
+    queues.open(queue);
+    for (;;) {
+        const int total = queues.total(queue);
+        if (k < total) {
+            const PrefillItem item = queues.find(queue, k);
+            // the next ticket is on its way meanwhile
+            unsigned next = 0;
+            if (tid == 0 && total > places)
+                next = __hip_atomic_fetch_add(p.control + kPfCtlTickets + queue, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            prefill_item<D>(p, sh, item);
+            __syncthreads();
+            if (tid == 0) sh.ticket = total > places ? places + (int)next : total;
+            __syncthreads();
+            k = sh.ticket;
+            continue;
+        }
+        // the others: only those with more items than workgroups that start on them
+        do {
+            queue = (queue + 1) % kPfQueues;
+            ++tried;
+        } while (tried < kPfQueues && queues.total(queue) <= places);
+        if (tried >= kPfQueues) break;
+        __syncthreads();
+        if (tid == 0)
+            sh.ticket = places + (int)__hip_atomic_fetch_add(p.control + kPfCtlTickets + queue, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        k = sh.ticket;
+        if (k < queues.total(queue)) queues.open(queue);
+    }
+    // the last workgroup to leave puts the tickets back
+    if (tid == 0) {
+        const unsigned gone = __hip_atomic_fetch_add(p.control + kPfCtlGone, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        if (gone == gridDim.x - 1) {
+            for (int y = 0; y < kPfQueues; ++y)
+                __hip_atomic_store(p.control + kPfCtlTickets + y, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(p.control + kPfCtlGone, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
 }
 
 }  // namespace hetis

@@ -247,6 +247,17 @@ def test_starts_past_the_rows():
     assert np.array_equal(bits(out)[:c.n], want[:c.n]) and (bits(out)[c.n:] == SENTINEL).all()
 
 
+@pytest.mark.parametrize("ahead,mb", [(200, None), (1000, None), (1000, 300)])
+def test_starts_that_do_not_begin_at_zero(ahead, mb):
+    """Rows ahead of the first sequence's, and tiles of theirs that belong to none."""
+    c = Case([100, 50, 140], [100, 50, 140], 2, 2, 64, seed=45, max_blocks=mb)
+    want = bits(c.run([0, 1]))
+    c.q = np.concatenate([np.zeros((ahead, 2, 64), dtype=np.float16), c.q])
+    c.starts, c.n = c.starts + ahead, c.n + ahead
+    got = bits(c.run([0, 1]))
+    assert np.array_equal(got[ahead:], want) and (got[:ahead] == SENTINEL).all()
+
+
 def test_two_streams_and_graphs():
     """Two captured calls with a workspace each, replayed side by side, between eager calls."""
     c = Case([6000, 130, 17], [40, 130, 1], 8, 2, 128, seed=51)

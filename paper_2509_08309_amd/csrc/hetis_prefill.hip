@@ -35,7 +35,7 @@ static PrefillLayout prefill_layout(const hetis_attn_shape *s, int32_t n_tokens,
 {
     PrefillLayout w;
     const int64_t steps = ((int64_t)s->max_blocks_per_seq * kBlockTokens + kPfStep - 1) / kPfStep;
-    const int64_t segs = std::min<int64_t>((steps + kPfOneTileSteps - 1) / kPfOneTileSteps, kPfSplitItems);
+    const int64_t segs = std::min<int64_t>((steps + kPfSegSteps - 1) / kPfSegSteps, kPfSplitItems);
     if (segs <= 1 || n_tokens == 0) return w;            // no row of the table is long enough
     // a row in every segment, or the items that a sequence can have: whichever is less
     const int64_t by_row = segs * n_tokens * (s->n_q_heads / s->n_kv_heads);
@@ -87,8 +87,11 @@ static int prefill_call(const hetis_attn_shape *shape, const void *q, const int3
     const int r = shape->n_q_heads / shape->n_kv_heads;
     p.group_shift = r == 8 ? 3 : r / 2;
     p.max_blocks_per_seq = shape->max_blocks_per_seq;
-    p.tiles = n_tokens / (kPfRows / r) + shape->batch;
-    if ((int64_t)p.tiles * n_sel > 1 << 30) return HETIS_ERR_UNSUPPORTED;
+    // numbers of a head: tiles, and what the sequences may have beside them
+    const int64_t gap = lay.rows ? 1 + kPfSplitItems : 1, numbers = n_tokens / (kPfRows / r) + gap * shape->batch;
+    if (numbers * n_sel > 1 << 30) return HETIS_ERR_UNSUPPORTED;
+    p.tiles = (int)numbers;
+    p.gap = (int)gap;
     p.scale_log2 = std::max(std::fabs(scale) * kLog2e, FLT_MIN);         // (0 times a masked score would be NaN)
     p.q_sign = std::signbit(scale) ? 0x80008000u : 0u;
     p.partial = reinterpret_cast<float *>(ws + lay.partial);
@@ -99,22 +102,20 @@ static int prefill_call(const hetis_attn_shape *shape, const void *q, const int3
     const int cus = device_cu_count();
     if (cus <= 0) return HETIS_ERR_LAUNCH;
     const int heads = heads_of_a_launch(shape, n_sel);
+    const bool direct = lay.rows == 0 || numbers * n_sel <= 4 * cus;
     for (int h = 0; h < n_sel; h += heads) {
         p.head_ids = head_ids + h;
         p.n_sel = std::min(heads, n_sel - h);
-        // two workgroups a compute unit, and no more than there can be items; whole rounds of the queues
-        const int64_t items = ((int64_t)p.tiles + (lay.rows ? (int64_t)shape->batch * kPfSplitItems : 0)) * p.n_sel;
-        if (lay.rows == 0 && items <= 2 * cus) {
-            if (shape->head_dim == 128) prefill_direct_kernel<128><<<(unsigned)items, kPfThreads, 0, st>>>(p);
-            else prefill_direct_kernel<64><<<(unsigned)items, kPfThreads, 0, st>>>(p);
-            rc = launched();
-            if (rc != HETIS_OK) return rc;
-            continue;
+        if (direct) {
+            const unsigned items = (unsigned)(p.tiles * p.n_sel);
+            if (shape->head_dim == 128) prefill_direct_kernel<128><<<items, kPfThreads, 0, st>>>(p);
+            else prefill_direct_kernel<64><<<items, kPfThreads, 0, st>>>(p);
+        } else {
+            // two workgroups a compute unit, in whole rounds of the queues
+            const dim3 places((unsigned)(2 * cus + kPfQueues - 1) / kPfQueues * kPfQueues);
+            if (shape->head_dim == 128) prefill_kernel<128><<<places, kPfThreads, 0, st>>>(p);
+            else prefill_kernel<64><<<places, kPfThreads, 0, st>>>(p);
         }
-        const int64_t grid = std::min<int64_t>(items, 2 * cus);
-        const dim3 places((unsigned)((grid + kPfQueues - 1) / kPfQueues * kPfQueues));
-        if (shape->head_dim == 128) prefill_kernel<128><<<places, kPfThreads, 0, st>>>(p);
-        else prefill_kernel<64><<<places, kPfThreads, 0, st>>>(p);
         rc = launched();
         if (rc != HETIS_OK) return rc;
     }

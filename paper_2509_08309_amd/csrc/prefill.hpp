@@ -40,7 +40,8 @@ struct PrefillParams {
     unsigned int *control, *arrivals;       // arrivals: [batch, n_sel, kPfSplitTiles]
     int64_t stride_block, stride_head;      // elements
     int64_t partial_rows;                   // of a head
-    int32_t n_tokens, batch, n_sel, n_q_heads, group_shift, max_blocks_per_seq, tiles;
+    int32_t n_tokens, batch, n_sel, n_q_heads, group_shift, max_blocks_per_seq;
+    int32_t tiles, gap;                     // direct launches: numbers of a head, see prefill_direct
     int32_t rows_by_sequence;               // partial rows are numbered by sequence and item, otherwise by segment and row
     float scale_log2;                       // the scale's magnitude
     uint32_t q_sign;                        // its sign, for the two query values of a word
@@ -51,22 +52,24 @@ constexpr int kPfThreads = 64 * kPfWaves;
 constexpr int kPfRows = 32 * kPfWaves;      // rows of a tile
 constexpr int kPfStep = 64;                 // cached tokens of a step
 // A sequence of few tiles over a long cache is cut along the cache as well, by its own numbers only: into at most
-// kPfSplitItems / tiles segments of at least kPfOneTileSteps or kPfFewTilesSteps steps.
-constexpr int kPfSplitTiles = 8, kPfSplitItems = 32, kPfOneTileSteps = 8, kPfFewTilesSteps = 16;
+// kPfSplitItems / tiles segments of at least kPfSegSteps steps.
+constexpr int kPfSplitTiles = 8, kPfSplitItems = 32, kPfSegSteps = 16;
 constexpr int kPfQueues = 8;
+constexpr int kPfBatch = 8;                 // segments that are added up at a time
 enum : int { kPfCtlTickets = 16, kPfCtlGone = 24 };      // control words: a queue's tickets, workgroups finished
 
 // What there is to do for a sequence.
 struct PrefillSequence {
-    int start, fresh, len, rows, tiles, segs, seg_steps;    // rows: tokens with a row; seg_steps: steps of a segment
+    int b, start, fresh, len, rows, tiles, segs, seg_steps; // rows: tokens with a row; seg_steps: steps of a segment
     __device__ __forceinline__ int items() const { return tiles * segs; }
 };
-__device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillParams &p, int start, int end, int len)
+__device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillParams &p, int b)
 {
     PrefillSequence s;
-    s.start = start;
-    s.fresh = end - start;
-    s.len = len;
+    s.b = b;
+    s.start = p.q_starts[b];
+    s.fresh = p.q_starts[b + 1] - s.start;
+    s.len = p.seq_lens[b];
     // (rows that q does not have are no work)
     s.rows = s.start < 0 || s.start >= p.n_tokens ? 0 : min(max(s.fresh, 0), p.n_tokens - s.start);
     const int steps = (min(max(s.len, 0), p.max_blocks_per_seq * kBlockTokens) + kPfStep - 1) / kPfStep;
@@ -74,8 +77,7 @@ __device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillParams 
     s.segs = 1;
     s.seg_steps = max(steps, 1);
     if (s.tiles >= 1 && s.tiles <= kPfSplitTiles) {
-        const int least = s.tiles == 1 ? kPfOneTileSteps : kPfFewTilesSteps;
-        const int want = min((steps + least - 1) / least, kPfSplitItems / s.tiles);
+        const int want = min((steps + kPfSegSteps - 1) / kPfSegSteps, kPfSplitItems / s.tiles);
         if (want > 1) {
             s.seg_steps = (steps + want - 1) / want;
             s.segs = (steps + s.seg_steps - 1) / s.seg_steps;
@@ -84,13 +86,8 @@ __device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillParams 
     return s;
 }
 
-__device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillParams &p, int b)
-{
-    return prefill_sequence(p, p.q_starts[b], p.q_starts[b + 1], p.seq_lens[b]);
-}
-
 struct PrefillItem {
-    int b, head, tile, seg;                 // head: place in head_ids
+    int head, tile, seg;                    // head: place in head_ids
     PrefillSequence seq;
 };
 
@@ -142,16 +139,53 @@ __device__ __forceinline__ int k_piece(int r, int c) { return c ^ (D == 128 ? r 
 template <int D>
 __device__ __forceinline__ int v_piece(int r, int c) { return c ^ (D == 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2); }
 
+// This thread's number, anew: what follows from it is worked out where it is used (kept over all items it was spilled).
+__device__ __forceinline__ int thread_here()
+{
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    return tid;
+}
+
+__device__ __forceinline__ void meet_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 template <int D>
 struct PrefillLds {
     unsigned char kv[2][2][kPfStep * D * 2];            // K, V; two steps
     int odd_from[3][D], any_odd;                        // first token with a value of +inf, -inf, NaN that some rows do not see
     int before[kPfThreads + 1];                         // items of a queue ahead of a thread's sequences
-    int order[kPfThreads], key[kPfThreads];             // sequences by their place, and what they are placed by
-    int starts[kPfThreads + 1], lens[kPfThreads];
+    __attribute__((aligned(16))) int key[kPfThreads];   // what the sequences are ordered by
+    PrefillSequence sequences[kPfThreads];              // by their place, up to one for each thread
     int sums[kPfWaves], totals[kPfWaves][kPfQueues];
-    int item[2], ticket, last;
+    PrefillItem item;
+    int ticket, last;
 };
+
+// 32 dims of a row over the row's sum of weights, sixteen in each of its two lanes (dims 8 j + 4 h ..): the lanes change
+// halves, and each stores twice eight dims.
+__device__ __forceinline__ void prefill_store(const float (&o)[16], float l, __half *to, bool there, int h)
+{
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+        unsigned w[2][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                const pf_f16x2 x = {(_Float16)(o[4 * (j + e) + 2 * f] * inv), (_Float16)(o[4 * (j + e) + 2 * f + 1] * inv)};
+                w[e][f] = __builtin_bit_cast(unsigned, x);
+            }
+        u32x4 x;
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const auto r = __builtin_amdgcn_permlane32_swap(w[0][f], w[1][f], false, false);
+            x[f] = r[0];
+            x[2 + f] = r[1];
+        }
+        if (there) *reinterpret_cast<u32x4 *>(to + 8 * (j + h)) = x;
+    }
+}
 
 template <int D>
 __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<D> &sh, const PrefillItem &item)
@@ -160,13 +194,12 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
     constexpr int DB = D / 32;              // row blocks of O^T
     constexpr int CH = D / 8;               // 16-byte pieces of a row
     constexpr int PER = D / 32;             // pieces of a page in a lane
-    int tid = threadIdx.x;
-    asm volatile("" : "+v"(tid));           // (what follows from it stays in here: kept over all items it was spilled)
+    const int tid = thread_here();
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, h = lane >> 5;
     // (scalar loads: a vector load would wait for what is on its way to LDS)
     typedef const __attribute__((address_space(4))) int32_t *Scalars;
-    const int b = item.b, g = reinterpret_cast<Scalars>(reinterpret_cast<uintptr_t>(p.head_ids))[item.head];
+    const int b = item.seq.b, g = reinterpret_cast<Scalars>(reinterpret_cast<uintptr_t>(p.head_ids))[item.head];
     const PrefillSequence &seq = item.seq;
     const int start = seq.start, fresh = seq.fresh, L = seq.len;
     const int t_first = item.tile << (7 - p.group_shift);               // tokens of a tile: 128 / r
@@ -200,10 +233,15 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
     const int from_v = lane / CH * (2 * D) + v_piece<D>(lane / CH, lane % CH) * 16;
 #pragma unroll
     for (int e = 0; e < PER; ++e) from_k[e] = lane / CH * (2 * D) + k_piece<D>(e * (64 / CH) + lane / CH, lane % CH) * 16;
-    auto bring = [&](int step, bool values) {
-        const int page = step * (kPfStep / kBlockTokens) + wave;
-        const int rows = min(max(seen - page * kBlockTokens, 0), kBlockTokens);
-        const int64_t block = table[min(page, pages - 1)];
+    // Block ids are asked for a step ahead of the loads that need them, by a vector load, so that the wait for the pages
+    // covers them (a scalar load on its way makes every LDS read wait for all the others).
+    int zero = 0;
+    asm volatile("" : "+v"(zero));
+    auto ask_id = [&](int step) {
+        return p.block_table[(int64_t)b * p.max_blocks_per_seq + min(step * (kPfStep / kBlockTokens) + wave, pages - 1) + zero];
+    };
+    auto bring = [&](int step, bool values, int64_t block) {
+        const int rows = min(max(seen - (step * (kPfStep / kBlockTokens) + wave) * kBlockTokens, 0), kBlockTokens);
         const i32x4 r = tile_descriptor((values ? p.v : p.k) + block * p.stride_block + head, rows * D * 2);
         const unsigned to = (unsigned)(uintptr_t)(LdsByte)&sh.kv[values][step & 1][wave * (kBlockTokens * D * 2)];
         if (values) page_to_lds<D>(r, from_v, from_v, from_v, from_v, to);
@@ -250,7 +288,14 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
         const int r = 4 * h + (lane >> 2 & 3), cc = lane & 3;
         v_at[d] = r * (2 * D) + v_piece<D>(r, 4 * d + 2 * (lane >> 4 & 1) + (cc >> 1)) * 16 + (cc & 1) * 8;
     }
-    if (first < steps) bring(first, false);
+    int block0 = 0, block1 = 0, asked = 0;              // of this wave's pages: the step at hand, the next, the one behind
+    if (first < steps) {
+        const int page = first * (kPfStep / kBlockTokens) + wave;
+        block0 = table[min(page, pages - 1)];
+        block1 = table[min(page + kPfStep / kBlockTokens, pages - 1)];
+        asked = ask_id(first + 2);
+        bring(first, false, block0);
+    }
     pf_f16x8 q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -365,8 +410,8 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
     if (first < steps) {
         drain();
         meet();
-        bring(first, true);
-        if (first + 1 < steps) bring(first + 1, false);
+        bring(first, true, block0);
+        if (first + 1 < steps) bring(first + 1, false, block1);
         if (first < own_steps) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -379,10 +424,13 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
     auto turn = [&](int step) {
         drain();
         clean(step);
+        const int block2 = __builtin_amdgcn_readfirstlane(asked);
         drain();
         meet();
-        if (step + 1 < steps) bring(step + 1, true);
-        if (step + 2 < steps) bring(step + 2, false);
+        if (step + 1 < steps) bring(step + 1, true, block1);
+        if (step + 2 < steps) bring(step + 2, false, block2);
+        block1 = block2;
+        if (step + 3 < steps) asked = ask_id(step + 3);
     };
     int step = first;
     for (; step < own_steps - 1; ++step) {
@@ -448,58 +496,57 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
         drain();
         meet();
         if (!sh.last) return;
-        if (n < wave_rows) {
-            mc = kNegBig;
-            l = 0.f;
+        // 32 rows by 32 dims a wave at a time, kPfBatch segments on their way
+        const int rows = (t_last + 1 - t_first) << p.group_shift, units = (rows + 31) / 32 * DB;
+#pragma clang loop unroll(disable)
+        for (int unit = wave; unit < units; unit += kPfWaves) {
+            const int group = unit / DB, d = unit % DB, of_group = min(rows - group * 32, 32);
+            float sum[16], m1 = kNegBig, l1 = 0.f;
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+            for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+#pragma clang loop unroll(disable)
+            for (int s0 = 0; s0 < tile_segs; s0 += kPfBatch) {
+                float m2[kPfBatch], l2[kPfBatch];
+                u32x4 x[kPfBatch][4];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-            for (int seg = 0; seg < tile_segs; ++seg) {
-                const float m2 = coherent_load(pairs_at(seg)), l2 = coherent_load(pairs_at(seg) + 1);
-                const __amdgpu_buffer_rsrc_t r = rows_at(seg);
-                const float to = fmaxf(mc, m2), was = fast_exp2(mc - to), is = fast_exp2(m2 - to);
-                mc = to;
-                l = __builtin_fmaf(l2, is, l * was);
+                for (int i = 0; i < kPfBatch; ++i) {
+                    const int64_t from = place(min(s0 + i, tile_segs - 1)) + (group - wave) * 32;
+                    const float *pair = p.partial + pairs + (from + min(n, of_group - 1)) * 2;
+                    m2[i] = coherent_load(pair);
+                    l2[i] = coherent_load(pair + 1);
+                    const __amdgpu_buffer_rsrc_t r = coherent_rsrc(p.partial + from * D, of_group * D * 4);
 #pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    u32x4 x[4];
+                    for (int j = 0; j < 4; ++j) x[i][j] = coherent_load_b128(r, ((2 * (4 * d + j) + h) * of_group + n) * 16, 0);
+                }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] = coherent_load_b128(r, ((2 * (4 * d + j) + h) * wave_rows + n) * 16, 0);
+                for (int i = 0; i < kPfBatch; ++i) {
+                    if (s0 + i >= tile_segs) break;
+                    const float to = fmaxf(m1, m2[i]), was = fast_exp2(m1 - to), is = fast_exp2(m2[i] - to);
+                    m1 = to;
+                    l1 = __builtin_fmaf(l2[i], is, l1 * was);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const f32x4 y = __builtin_bit_cast(f32x4, x[j]);
+                        const f32x4 y = __builtin_bit_cast(f32x4, x[i][j]);
 #pragma unroll
-                        for (int f = 0; f < 4; ++f) o[d][4 * j + f] = __builtin_fmaf(y[f], is, o[d][4 * j + f] * was);
+                        for (int f = 0; f < 4; ++f) sum[4 * j + f] = __builtin_fmaf(y[f], is, sum[4 * j + f] * was);
                     }
                 }
             }
+            const int row1 = group * 32 + n;
+            const int64_t at1 = (int64_t)start + t_first + (row1 >> p.group_shift);
+            __half *to = p.out + (at1 * p.n_q_heads + ((int64_t)g << p.group_shift) + (row1 & ((1 << p.group_shift) - 1))) * D;
+            prefill_store(sum, l1, to + 32 * d, n < of_group, h);
         }
+        return;
     }
 
-    const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d) {
+        float sum[16];
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-            // lanes h = 0 and 1 hold dims 8 j + 4 h ..: they change halves, and each stores eight dims
-            unsigned w[2][2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    const pf_f16x2 x = {(_Float16)(o[d][4 * (j + e) + 2 * f] * inv), (_Float16)(o[d][4 * (j + e) + 2 * f + 1] * inv)};
-                    w[e][f] = __builtin_bit_cast(unsigned, x);
-                }
-            u32x4 x;
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                const auto r = __builtin_amdgcn_permlane32_swap(w[0][f], w[1][f], false, false);
-                x[f] = r[0];
-                x[2 + f] = r[1];
-            }
-            if (there) *reinterpret_cast<u32x4 *>(p.out + element + 32 * d + 8 * (j + h)) = x;
-        }
+        for (int e = 0; e < 16; ++e) sum[e] = o[d][e];
+        prefill_store(sum, l, p.out + element + 32 * d, there, h);
+    }
 }
 
 // The sequences, longest items first, and their items in kPfQueues queues: (sequence, head) number i belongs to queue i
@@ -509,7 +556,7 @@ template <int D>
 struct PrefillQueues {
     const PrefillParams &p;
     PrefillLds<D> &sh;
-    int per, mine;                          // sequences a thread looks after; items a head of its first one
+    int per;                                // sequences that a thread looks after
 
     __device__ __forceinline__ int pairs_in(int queue, int rank, int *first_head) const
     {
@@ -517,32 +564,29 @@ struct PrefillQueues {
         *first_head = h0;
         return h0 < p.n_sel ? (p.n_sel - 1 - h0) / kPfQueues + 1 : 0;
     }
-    __device__ __forceinline__ PrefillSequence sequence(int b) const
-    {
-        return per == 1 ? prefill_sequence(p, sh.starts[b], sh.starts[b + 1], sh.lens[b]) : prefill_sequence(p, b);
-    }
-
     __device__ __forceinline__ PrefillQueues(const PrefillParams &p_, PrefillLds<D> &sh_) : p(p_), sh(sh_)
     {
         const int tid = threadIdx.x;
         per = (p.batch + kPfThreads - 1) / kPfThreads;
-        mine = 0;
         if (per == 1) {
             // by the steps of an item, descending (few sequences: each thread compares with all)
+            PrefillSequence s{};
+            int key = -1;
             if (tid < p.batch) {
-                sh.starts[tid] = p.q_starts[tid];
-                sh.lens[tid] = p.seq_lens[tid];
-                if (tid == p.batch - 1) sh.starts[p.batch] = p.q_starts[p.batch];
+                s = prefill_sequence(p, tid);
+                key = s.seg_steps;
             }
-            __syncthreads();
-            const int key = tid < p.batch ? sequence(tid).seg_steps : -1;
             sh.key[tid] = key;
             __syncthreads();
             int rank = 0;
-            for (int j = 0; j < p.batch; ++j) rank += sh.key[j] > key || (sh.key[j] == key && j < tid);
-            if (tid < p.batch) sh.order[rank] = tid;
+#pragma unroll 4
+            for (int j = 0; j < p.batch; j += 4) {
+                const i32x4 k = *reinterpret_cast<const i32x4 *>(&sh.key[j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) rank += k[e] > key || (k[e] == key && j + e < tid);
+            }
+            if (tid < p.batch) sh.sequences[rank] = s;
             __syncthreads();
-            if (tid < p.batch) mine = sequence(sh.order[tid]).items();
         }
         // items of every queue
         int total[kPfQueues] = {};
@@ -564,11 +608,12 @@ struct PrefillQueues {
     template <class F>
     __device__ __forceinline__ void each(F f) const
     {
+        const int tid = thread_here();
         if (per == 1) {
-            if ((int)threadIdx.x < p.batch) f((int)threadIdx.x, mine);
+            if (tid < p.batch) f(tid, sh.sequences[tid].items());
             return;
         }
-        for (int i = 0, rank = threadIdx.x * per; i < per && rank < p.batch; ++i, ++rank) f(rank, prefill_sequence(p, rank).items());
+        for (int i = 0, rank = tid * per; i < per && rank < p.batch; ++i, ++rank) f(rank, prefill_sequence(p, rank).items());
     }
     __device__ __forceinline__ int total(int queue) const
     {
@@ -580,7 +625,7 @@ struct PrefillQueues {
     // items of the queue ahead of each thread's
     __device__ __forceinline__ void open(int queue)
     {
-        const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+        const int tid = thread_here(), lane = tid % 64, wave = tid / 64;
         int sum = 0, h0;
         each([&](int rank, int items) { sum += items * pairs_in(queue, rank, &h0); });
         int upto = sum;
@@ -600,58 +645,57 @@ struct PrefillQueues {
     // Item k of the open queue: of a sequence the tiles that see most first, one for each head.
     __device__ __forceinline__ PrefillItem find(int queue, int k)
     {
-        const int tid = threadIdx.x;
+        const int tid = thread_here();
         if (sh.before[tid] <= k && k < sh.before[tid + 1]) {
             int rem = k - sh.before[tid], h0;
             for (int rank = tid * per; rank < p.batch; ++rank) {
-                const int items = (per == 1 ? mine : prefill_sequence(p, rank).items()) * pairs_in(queue, rank, &h0);
+                const PrefillSequence s = per == 1 ? sh.sequences[rank] : prefill_sequence(p, rank);
+                const int pairs = pairs_in(queue, rank, &h0), items = s.items() * pairs;
                 if (rem < items) {
-                    sh.item[0] = rank;
-                    sh.item[1] = rem;
+                    const unsigned u = (unsigned)rem / (unsigned)pairs, tile = u / (unsigned)s.segs;
+                    sh.item.head = h0 + kPfQueues * (rem - (int)u * pairs);
+                    sh.item.tile = s.tiles - 1 - (int)tile;
+                    sh.item.seg = (int)(u - tile * s.segs);
+                    sh.item.seq = s;
                     break;
                 }
                 rem -= items;
             }
         }
-        __syncthreads();
-        const int rank = __builtin_amdgcn_readfirstlane(sh.item[0]), rem = __builtin_amdgcn_readfirstlane(sh.item[1]);
+        meet_lds();
+        // (the same for every thread: into scalar registers)
         PrefillItem item;
-        item.b = per == 1 ? __builtin_amdgcn_readfirstlane(sh.order[rank]) : rank;
-        if (per == 1)
-            item.seq = prefill_sequence(p, __builtin_amdgcn_readfirstlane(sh.starts[item.b]),
-                                        __builtin_amdgcn_readfirstlane(sh.starts[item.b + 1]), __builtin_amdgcn_readfirstlane(sh.lens[item.b]));
-        else
-            item.seq = prefill_sequence(p, item.b);
-        int h0;
-        const int pairs = pairs_in(queue, rank, &h0), u = rem / pairs;
-        item.head = h0 + kPfQueues * (rem % pairs);
-        item.tile = item.seq.tiles - 1 - u / item.seq.segs;
-        item.seg = u % item.seq.segs;
+        constexpr int WORDS = sizeof(PrefillItem) / sizeof(int);
+        const int *from = reinterpret_cast<const int *>(&sh.item);
+        int *to = reinterpret_cast<int *>(&item);
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) to[w] = __builtin_amdgcn_readfirstlane(from[w]);
         return item;
     }
 };
 
-// A launch of few items, none of them cut along the cache: item i is workgroup i's, and nothing is handed out.  Tile
-// numbers are q_starts[b] / tokens + b + the tile's place in its sequence b (tokens: of a tile), which leaves at least as
-// many numbers to a sequence as it has tiles; the sequence of a number is found 64 starts at a time.
+// A launch without sequences that are cut along the cache, or of few items: item i is workgroup i's, and nothing is handed
+// out.  Items are numbered from q_starts[b] / tokens + gap b on (tokens: of a tile), which leaves at least as many numbers
+// to a sequence as it has items if the gap is what it may have beside its tiles; the sequence of a number is found 64
+// starts at a time.
 __device__ __forceinline__ PrefillItem prefill_direct(const PrefillParams &p, int number)
 {
-    const int lane = threadIdx.x % 64, token_shift = 7 - p.group_shift, tile = p.tiles - 1 - number / p.n_sel;
+    const int lane = threadIdx.x % 64, token_shift = 7 - p.group_shift, place = p.tiles - 1 - number / p.n_sel;
     int lo = 0, n = p.batch;                // the answer is in [lo, lo + n)
     while (n > 1) {
         const int step = (n + 63) / 64;
         const int b = lo + lane * step;
-        const bool ok = lane * step < n && (max(p.q_starts[min(b, p.batch)], 0) >> token_shift) + b <= tile;
+        const bool ok = lane * step < n && (max(p.q_starts[min(b, p.batch)], 0) >> token_shift) + b * p.gap <= place;
         const int found = max((int)__popcll(__ballot(ok)) - 1, 0);          // (a count is unsigned)
         lo += found * step;
         n = min(step, n - found * step);
     }
     PrefillItem item;
-    item.b = __builtin_amdgcn_readfirstlane(lo);
     item.head = number % p.n_sel;
-    item.seq = prefill_sequence(p, item.b);
-    item.tile = tile - (max(item.seq.start, 0) >> token_shift) - item.b;
-    item.seg = 0;
+    item.seq = prefill_sequence(p, __builtin_amdgcn_readfirstlane(lo));
+    const int u = place - (max(item.seq.start, 0) >> token_shift) - item.seq.b * p.gap;
+    item.tile = u < 0 ? -1 : u / item.seq.segs;
+    item.seg = u < 0 ? 0 : u % item.seq.segs;
     return item;
 }
 
@@ -680,10 +724,9 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_kernel(PrefillParams p)
             if (tid == 0 && total > places)
                 next = __hip_atomic_fetch_add(p.control + kPfCtlTickets + queue, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             prefill_item<D>(p, sh, item);
-            __syncthreads();
             if (tid == 0) sh.ticket = total > places ? places + (int)next : total;
-            __syncthreads();
-            k = sh.ticket;
+            meet_lds();                                 // (the item's results may still be on their way out)
+            k = __builtin_amdgcn_readfirstlane(sh.ticket);
             continue;
         }
         // the others: only those with more items than workgroups that start on them

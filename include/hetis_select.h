@@ -20,8 +20,8 @@
  * page of scale +inf scores +inf; a query head with an infinite value or NaN takes no part (a group of such
  * heads only: all pages score alike).
  *
- * Conventions: those of hetis_attn.h.  batch <= 65535, n_kv_heads <= 1024, max_blocks_per_seq <= 2^24; r in
- * {1, 2, 4, 8}; head_dim in {64, 128}; block_size 16.  Codes start at a 16-byte boundary.
+ * Conventions: those of hetis_attn.h.  batch <= 65535, n_kv_heads <= 1024, max_blocks_per_seq <= 2^24
+ * (hetis_kv_select: 2^23); hetis_kv_select: r in {1, 2, 4, 8}; head_dim in {64, 128}; block_size 16.  Codes start at a 16-byte boundary.
  */
 #ifndef HETIS_SELECT_H
 #define HETIS_SELECT_H

@@ -26,6 +26,7 @@ static int check_select_shape(const hetis_attn_shape *s, int32_t n_sel, CacheStr
     if (rc != HETIS_OK) return rc;
     const int r = s->n_q_heads / s->n_kv_heads;
     if (r != 1 && r != 2 && r != 4 && r != 8) return HETIS_ERR_UNSUPPORTED;
+    if (s->max_blocks_per_seq > 1 << 23) return HETIS_ERR_UNSUPPORTED;   // a grid's limit in y
     const int64_t tile = (int64_t)2 * kBlockTokens * s->head_dim;
     return c->block % tile == 0 && c->head % tile == 0 ? HETIS_OK : HETIS_ERR_BAD_SHAPE;
 }
@@ -67,13 +68,18 @@ static int select_call(const hetis_attn_shape *shape, const void *q, const void 
     p.n_sink = n_sink;
     p.n_recent = n_recent;
     if (shape->max_blocks_per_seq > n_pages) {
-        const dim3 grid((unsigned)((shape->max_blocks_per_seq + kScorePages - 1) / kScorePages), (unsigned)n_sel, (unsigned)shape->batch);
+        const dim3 grid((unsigned)n_sel, (unsigned)((shape->max_blocks_per_seq + kScorePages - 1) / kScorePages), (unsigned)shape->batch);
         if (shape->head_dim == 128) score_kernel<128><<<grid, kScoreThreads, 0, st>>>(p);
         else score_kernel<64><<<grid, kScoreThreads, 0, st>>>(p);
         rc = launched();
         if (rc != HETIS_OK) return rc;
     }
-    select_kernel<<<dim3((unsigned)n_sel, (unsigned)shape->batch), kSelectThreads, 0, st>>>(p);
+    // keys in registers where a row of the table fits
+    const dim3 rows((unsigned)n_sel, (unsigned)shape->batch);
+    const int pages = shape->max_blocks_per_seq;
+    if (pages <= kSelectThreads * 2) select_kernel<2, true><<<rows, kSelectThreads, 0, st>>>(p);
+    else if (pages <= kSelectThreads * 8) select_kernel<8, true><<<rows, kSelectThreads, 0, st>>>(p);
+    else select_kernel<8, false><<<rows, kSelectThreads, 0, st>>>(p);
     return launched();
 }
 
@@ -114,10 +120,10 @@ int hetis_kv_bounds(const hetis_attn_shape *shape, const void *k_cache, const in
         return shape->head_dim == 128 ? launch_kv(bounds_kernel<128, true>, grid, st, p)
                                       : launch_kv(bounds_kernel<64, true>, grid, st, p);
     }
-    // a wave a page, up to some forty workgroups for each place of a compute unit; longer rows stride on
-    const int64_t rows = (int64_t)shape->batch * n_sel_heads;
+    // kBoundsPages pages a wave, up to 2^16 workgroups; longer rows stride on
+    const int64_t rows = (int64_t)shape->batch * n_sel_heads, per_wg = waves * kBoundsPages;
     const int64_t most = std::max<int64_t>(((int64_t)1 << 16) / rows, 1);
-    const dim3 grid((unsigned)std::min<int64_t>((shape->max_blocks_per_seq + waves - 1) / waves, most), (unsigned)n_sel_heads,
+    const dim3 grid((unsigned)n_sel_heads, (unsigned)std::min<int64_t>({(shape->max_blocks_per_seq + per_wg - 1) / per_wg, most, 65535}),
                     (unsigned)shape->batch);
     return shape->head_dim == 128 ? launch_kv(bounds_kernel<128, false>, grid, st, p)
                                   : launch_kv(bounds_kernel<64, false>, grid, st, p);

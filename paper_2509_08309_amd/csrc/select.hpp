@@ -11,7 +11,6 @@
 namespace hetis {
 
 typedef _Float16 sel_f16x2 __attribute__((ext_vector_type(2)));
-typedef unsigned short sel_u16x2 __attribute__((ext_vector_type(2)));
 
 struct BoundsParams {
     const unsigned char *k;                 // fp16 tiles
@@ -30,12 +29,10 @@ __device__ __forceinline__ uint2 lanes_xor(unsigned x)
     if constexpr (M == 32) {
         const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
         return make_uint2(r[0], r[1]);
-    } else if constexpr (M == 16) {
+    } else {
+        static_assert(M == 16, "a swap of neighbouring rows or of halves");
         const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
         return make_uint2(r[0], r[1]);
-    } else {
-        static_assert(M == 8, "a turn of half a row");
-        return make_uint2(x, __builtin_amdgcn_update_dpp(0, x, 0x128, 0xF, 0xF, true));
     }
 }
 
@@ -45,93 +42,110 @@ __device__ __forceinline__ unsigned dpp_u32(unsigned x)
     return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, true);
 }
 
-constexpr int kBoundsThreads = 256;
+// Four words of two halves each (the same eight dims in lanes 16 and 32 apart, and 8 apart where 8 lanes hold a row), over
+// those lanes: a swap puts two words' halves of the lanes side by side, so that one operation folds both.  Lane l ends
+// up with word l / 32 + 2 (l / 16 % 2).
+template <int D, bool MAX>
+__device__ __forceinline__ unsigned fold_words(const unsigned (&x)[4])
+{
+    auto both = [](unsigned a, unsigned b) {
+        const sel_f16x2 u = __builtin_bit_cast(sel_f16x2, a), v = __builtin_bit_cast(sel_f16x2, b);
+        return __builtin_bit_cast(unsigned, MAX ? __builtin_elementwise_maximum(u, v) : __builtin_elementwise_minimum(u, v));
+    };
+    const auto p = __builtin_amdgcn_permlane32_swap(x[0], x[1], false, false);
+    const auto q = __builtin_amdgcn_permlane32_swap(x[2], x[3], false, false);
+    const auto r = __builtin_amdgcn_permlane16_swap(both(p[0], p[1]), both(q[0], q[1]), false, false);
+    unsigned w = both(r[0], r[1]);
+    if (D == 64) w = both(w, dpp_u32<0x128>(w));
+    return w;
+}
 
-// A wave a page: D / 8 lanes a row, sixteen bytes each; largest, smallest and largest magnitude (as whole numbers,
-// where infinity and NaN come last) are folded over a lane's rows and then over the lanes that hold the same dims.
-// Bound by the rows it reads.  LAST: the wave's number is a head's, and its page the sequence's last.
+constexpr int kBoundsThreads = 256;
+constexpr int kBoundsPages = 4;             // pages of a wave at a time, their rows all on their way
+
+// D / 8 lanes a row, sixteen bytes each; largest, smallest and largest magnitude (as whole numbers, where infinity and NaN
+// come last) are folded over a lane's rows and then over the lanes that hold the same dims.  Bound by the rows that it
+// reads.  LAST: the wave's number is a head's, and its page the sequence's last.
 template <int D, bool LAST>
 __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(BoundsParams p)
 {
-    constexpr int LR = D / 8, ROWS = 64 / LR, PASSES = kBlockTokens / ROWS;
+    constexpr int LR = D / 8, ROWS = 64 / LR, PASSES = kBlockTokens / ROWS, PAGES = LAST ? 1 : kBoundsPages;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), lane = threadIdx.x % 64;
-    const int unit = blockIdx.x * (kBoundsThreads / 64) + wave;
+    const int unit = (LAST ? blockIdx.x : blockIdx.y) * (kBoundsThreads / 64) + wave;
     const int64_t b = blockIdx.z;
-    const int i = LAST ? unit : (int)blockIdx.y;
+    const int i = LAST ? unit : (int)blockIdx.x;
     if (i >= p.n_sel) return;
     const int g = p.head_ids[i];
     const int L = min(p.seq_lens[b], p.max_blocks_per_seq * kBlockTokens);
     if (L <= 0 || g < 0 || g >= p.n_kv_heads) return;
     const int pages = (L + kBlockTokens - 1) / kBlockTokens;
-    const int first = LAST ? pages - 1 : max(p.first_pos[b], 0) / kBlockTokens + unit;
-    const int c = lane % LR, row = lane / LR;
-    for (int64_t page = first; page < pages; page += (int64_t)gridDim.x * (kBoundsThreads / 64)) {
-        const int64_t block = p.block_table[b * p.max_blocks_per_seq + page];
-        if (block < 0 || block >= p.num_blocks) continue;
-        const int64_t rest = L - page * kBlockTokens;
-        const int n = rest < kBlockTokens ? (int)rest : kBlockTokens;
-        const u32x4 *tile = reinterpret_cast<const u32x4 *>(p.k + block * p.stride_block + g * p.stride_head);
-        u32x4 x[PASSES];
+    const int first = LAST ? pages - 1 : max(p.first_pos[b], 0) / kBlockTokens + unit * PAGES;
+    const int c = lane % LR, row = lane / LR, word = lane >> 5 | (lane >> 4 & 1) << 1;
+    const int32_t *table = p.block_table + b * p.max_blocks_per_seq;
+    for (int64_t page0 = first; page0 < pages; page0 += (int64_t)gridDim.y * (kBoundsThreads / 64 * PAGES)) {
+        int64_t block[PAGES];
+        u32x4 rows[PAGES][PASSES];
 #pragma unroll
-        for (int e = 0; e < PASSES; ++e) x[e] = tile[min(e * ROWS + row, n - 1) * LR + c];   // (a row twice changes nothing)
-        unsigned hi[4], lo[4], mag[4];
+        for (int k = 0; k < PAGES; ++k) block[k] = table[min(page0 + k, (int64_t)pages - 1)];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const unsigned x0 = x[0][w];                           // (a bit cast of an element takes the vector's first)
-            sel_f16x2 h = __builtin_bit_cast(sel_f16x2, x0), l = h;
-            sel_u16x2 m = __builtin_bit_cast(sel_u16x2, x0 & 0x7fff7fffu);
+        for (int k = 0; k < PAGES; ++k) {
+            // (a row that is read twice changes nothing)
+            if (page0 + k >= pages || block[k] < 0 || block[k] >= p.num_blocks) block[k] = -1;
+            const int rest = L - (int)min(page0 + k, (int64_t)pages - 1) * kBlockTokens;
+            const int n = rest < kBlockTokens ? rest : kBlockTokens;
+            if (block[k] < 0) continue;
+            const u32x4 *tile = reinterpret_cast<const u32x4 *>(p.k + block[k] * p.stride_block + g * p.stride_head);
 #pragma unroll
-            for (int e = 1; e < PASSES; ++e) {
-                const unsigned xe = x[e][w];
-                const sel_f16x2 v = __builtin_bit_cast(sel_f16x2, xe);
-                h = __builtin_elementwise_max(h, v);
-                l = __builtin_elementwise_min(l, v);
-                m = __builtin_elementwise_max(m, __builtin_bit_cast(sel_u16x2, xe & 0x7fff7fffu));
-            }
-            hi[w] = __builtin_bit_cast(unsigned, h);
-            lo[w] = __builtin_bit_cast(unsigned, l);
-            mag[w] = __builtin_bit_cast(unsigned, m);
+            for (int e = 0; e < PASSES; ++e) rows[k][e] = __builtin_nontemporal_load(&tile[min(e * ROWS + row, n - 1) * LR + c]);
         }
-        auto fold = [&](auto mask) {
-            constexpr int M = decltype(mask)::value;
+#pragma unroll
+        for (int k = 0; k < PAGES; ++k) {
+            if (block[k] < 0) continue;
+            // largest and smallest of a lane's rows, NaN where there is one
+            unsigned hi[4], lo[4];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const uint2 a = lanes_xor<M>(hi[w]), z = lanes_xor<M>(lo[w]), m = lanes_xor<M>(mag[w]);
-                hi[w] = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(sel_f16x2, a.x), __builtin_bit_cast(sel_f16x2, a.y)));
-                lo[w] = __builtin_bit_cast(unsigned, __builtin_elementwise_min(__builtin_bit_cast(sel_f16x2, z.x), __builtin_bit_cast(sel_f16x2, z.y)));
-                mag[w] = __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(sel_u16x2, m.x), __builtin_bit_cast(sel_u16x2, m.y)));
-            }
-        };
-        if constexpr (D == 64) fold(std::integral_constant<int, 8>());
-        fold(std::integral_constant<int, 16>());
-        fold(std::integral_constant<int, 32>());
-        unsigned most = 0;
+                const unsigned x0 = rows[k][0][w];                 // (a bit cast of an element takes the vector's first)
+                sel_f16x2 h = __builtin_bit_cast(sel_f16x2, x0), l = h;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) most = max(most, max(mag[w] & 0xffffu, mag[w] >> 16));
-        most = max(most, dpp_u32<0xB1>(most));
-        most = max(most, dpp_u32<0x4E>(most));
-        most = max(most, dpp_u32<0x141>(most));
-        if (D == 128) most = max(most, dpp_u32<0x140>(most));
-        const bool finite = most < 0x7c00u;
-        const float s = finite ? (float)__builtin_bit_cast(_Float16, (unsigned short)most) * (1.f / 127.f) : INFINITY;
-        // lanes 4 LR: upper and lower codes of four dims each
-        const int part = lane / LR, lower = part & 1, at = part >> 1;
-        if (part < 4) {
-            unsigned word = 0;
+                for (int e = 1; e < PASSES; ++e) {
+                    const unsigned xe = rows[k][e][w];
+                    h = __builtin_elementwise_maximum(h, __builtin_bit_cast(sel_f16x2, xe));
+                    l = __builtin_elementwise_minimum(l, __builtin_bit_cast(sel_f16x2, xe));
+                }
+                hi[w] = __builtin_bit_cast(unsigned, h);
+                lo[w] = __builtin_bit_cast(unsigned, l);
+            }
+            const unsigned top = fold_words<D, true>(hi), low = fold_words<D, false>(lo);
+            unsigned most = max(max(top & 0x7fffu, top >> 16 & 0x7fffu), max(low & 0x7fffu, low >> 16 & 0x7fffu));
+            most = max(most, dpp_u32<0xB1>(most));
+            most = max(most, dpp_u32<0x4E>(most));
+            most = max(most, dpp_u32<0x141>(most));
+            most = max(most, dpp_u32<0x140>(most));
+            const uint2 m16 = lanes_xor<16>(most);
+            most = max(m16.x, m16.y);
+            const uint2 m32 = lanes_xor<32>(most);
+            most = max(m32.x, m32.y);
+            const bool finite = most < 0x7c00u;
+            const float s = finite ? (float)__builtin_bit_cast(_Float16, (unsigned short)most) * (1.f / 127.f) : INFINITY;
+            // a lane has two dims of each row of codes
+            unsigned up = 0, down = 0;
             if (finite && s > 0.f) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const unsigned h = at ? hi[2 + e / 2] : hi[e / 2], l = at ? lo[2 + e / 2] : lo[e / 2];
-                    const unsigned v = (lower ? l : h) >> (e % 2 * 16);
-                    const float q = (float)__builtin_bit_cast(_Float16, (unsigned short)v) / s;
-                    const int code = (int)(lower ? fmaxf(floorf(q), -127.f) : fminf(ceilf(q), 127.f));
-                    word |= (unsigned)(code & 255) << (8 * e);
+                for (int e = 0; e < 2; ++e) {
+                    const float h = (float)__builtin_bit_cast(_Float16, (unsigned short)(top >> (16 * e))) / s;
+                    const float l = (float)__builtin_bit_cast(_Float16, (unsigned short)(low >> (16 * e))) / s;
+                    up |= (unsigned)((int)fminf(ceilf(h), 127.f) & 255) << (8 * e);
+                    down |= (unsigned)((int)fmaxf(floorf(l), -127.f) & 255) << (8 * e);
                 }
             }
-            signed char *row_of = p.codes + ((block * p.n_kv_heads + g) * 2 + lower) * D;
-            *reinterpret_cast<unsigned *>(row_of + c * 8 + at * 4) = word;
+            if (D == 128 || (lane & 8) == 0) {
+                signed char *of = p.codes + (block[k] * p.n_kv_heads + g) * (2 * D) + c * 8 + word * 2;
+                *reinterpret_cast<unsigned short *>(of) = (unsigned short)up;
+                *reinterpret_cast<unsigned short *>(of + D) = (unsigned short)down;
+            }
+            if (lane == 0) p.scales[block[k] * p.n_kv_heads + g] = s;
         }
-        if (lane == 0) p.scales[block * p.n_kv_heads + g] = s;
     }
 }
 
@@ -166,13 +180,26 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(SelectParams p)
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64), lane = threadIdx.x % 64;
     const int n = lane & 15, quarter = lane >> 4;
     const int64_t b = blockIdx.z;
-    const int i = blockIdx.y;
+    const int i = blockIdx.x;
     const int L = min(max(p.seq_lens[b], 0), p.max_blocks_per_seq * kBlockTokens), pages = (L + kBlockTokens - 1) / kBlockTokens;
-    const int first = blockIdx.x * kScorePages;
+    const int first = blockIdx.y * kScorePages;
     if (pages <= p.n_pages || first >= pages) return;              // (all of them: nothing to score)
     const int g = p.head_ids[i];
+    // the wave's pages: one id a lane, then all their codes
+    const int at = first + wave * 64;
+    const int mine = p.block_table[b * p.max_blocks_per_seq + min(at + lane, pages - 1)];
+    const float s_mine = p.scales[(int64_t)mine * p.n_kv_heads + g];
+    i32x4 code[4][STEPS];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const signed char *page = p.codes + ((int64_t)__shfl(mine, 16 * k + n) * p.n_kv_heads + g) * (2 * D) + quarter * 16;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) code[k][s] = *reinterpret_cast<const i32x4 *>(page + 64 * s);
+    }
 
-    // the head's codes
+    // the head's codes: a wave works out a quarter of them (the divisions would take longer than the pages)
+    constexpr int WORDS = DIMS / 4;                                // of four codes, in a lane
+    __shared__ __attribute__((aligned(16))) unsigned shared[2][64][WORDS];
     float t = 0.f;
     bool counts = n < p.group;
     i32x4 query[STEPS];
@@ -195,33 +222,32 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(SelectParams p)
         counts = counts && most < 0x7c00u;
         t = (float)__builtin_bit_cast(_Float16, (unsigned short)most) * (1.f / 127.f);
 #pragma unroll
-        for (int w = 0; w < DIMS / 4; ++w) {                       // four codes a word
+        for (int w = 0; w < WORDS; ++w) {
+            if (w / (WORDS / 4) != wave) continue;
             unsigned up = 0, down = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const unsigned short bits = (unsigned short)(raw[2 * w + e / 2] >> (e % 2 * 16));
                 const float x = (float)__builtin_bit_cast(_Float16, bits);
-                const int code = counts && t > 0.f ? (int)rintf(x / t) : 0;
-                up |= (unsigned)max(code, 0) << (8 * e);
-                down |= (unsigned)(min(code, 0) & 255) << (8 * e);
+                const int c = counts && t > 0.f ? (int)rintf(x / t) : 0;
+                up |= (unsigned)max(c, 0) << (8 * e);
+                down |= (unsigned)(min(c, 0) & 255) << (8 * e);
             }
-            query[w / 4][w % 4] = (int)up;
-            query[w / 4 + STEPS / 2][w % 4] = (int)down;
+            shared[0][lane][w] = up;
+            shared[1][lane][w] = down;
         }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            query[s] = *reinterpret_cast<const i32x4 *>(&shared[s / (STEPS / 2)][lane][s % (STEPS / 2) * 4]);
     }
     unsigned *keys = p.keys + (b * p.n_sel + i) * p.max_blocks_per_seq;
-    const int32_t *table = p.block_table + b * p.max_blocks_per_seq;
-    for (int at = first + wave * 16; at < min(first + kScorePages, pages); at += kScoreThreads / 64 * 16) {
-        const int64_t mine = table[min(at + n, pages - 1)];        // (lanes past the end repeat the last page)
-        const signed char *page = p.codes + (mine * p.n_kv_heads + g) * (2 * D) + quarter * 16;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
         i32x4 acc = {0, 0, 0, 0};
-        i32x4 code[STEPS];
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) code[s] = *reinterpret_cast<const i32x4 *>(page + 64 * s);
-        const float s_mine = p.scales[mine * p.n_kv_heads + g];
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(code[s], query[s], acc, 0, 0, 0);
-        // lane (n, quarter): head n, pages at + 4 quarter + e
+        for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(code[k][s], query[s], acc, 0, 0, 0);
+        // lane (n, quarter): head n, pages at + 16 k + 4 quarter + e
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float best = counts ? (float)acc[e] * t : -INFINITY;
@@ -229,17 +255,22 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(SelectParams p)
             best = fmaxf(best, dpp_mov<0x4E>(best));
             best = fmaxf(best, dpp_mov<0x141>(best));
             best = fmaxf(best, dpp_mov<0x140>(best));
-            const int of = at + quarter * 4 + e;
-            const float s = __shfl(s_mine, quarter * 4 + e);
+            const int of = 16 * k + quarter * 4 + e;
+            const float s = __shfl(s_mine, of);
             const float score = s == INFINITY ? s : best == -INFINITY ? best : best * s;
-            if (n == 0 && of < pages)
-                keys[of] = of < p.n_sink || of >= pages - p.n_recent ? kSelectAlways : select_key(score);
+            if (n == 0 && at + of < pages)
+                keys[at + of] = at + of < p.n_sink || at + of >= pages - p.n_recent ? kSelectAlways : select_key(score);
         }
     }
 }
 
-constexpr int kSelectThreads = 512;
+constexpr int kSelectThreads = 1024;
 constexpr int kSelectBins = 2048;
+
+__device__ __forceinline__ int lanes_below(unsigned long long mask)
+{
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
+}
 
 // Sum of x over the threads before this one; the sum of all in *total.
 __device__ __forceinline__ unsigned long long threads_before(unsigned long long x, unsigned long long *sums, unsigned long long *total)
@@ -265,13 +296,18 @@ __device__ __forceinline__ unsigned long long threads_before(unsigned long long 
     return before;
 }
 
-// The n_pages pages of the largest keys of a row, ascending: the smallest of them by a radix selection from the top
-// (11, 11 and 10 bits), then a sweep in page order.  Counts are whole numbers: the same run to run.
+// The n_pages pages of the largest keys of a row, ascending: the smallest of them by a radix selection, then a sweep in
+// page order.  Counts are whole numbers: the same run to run.  Digits are of 11 bits from the highest bit on that the
+// keys' range has: scores lie within an octave or two, and digits of the bits as they are would crowd into a few
+// counters.  A thread keeps KEYS pages, kSelectThreads apart, of a window; ONE: the rows have one window, and keys are read
+// once.
+template <int KEYS, bool ONE>
 __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
 {
-    constexpr int PER = kSelectBins / kSelectThreads;
+    constexpr int PER = kSelectBins / kSelectThreads, WINDOW = kSelectThreads * KEYS;
     __shared__ int hist[kSelectBins];
     __shared__ unsigned long long sums[kSelectThreads / 64];
+    __shared__ unsigned long long counts[KEYS * (kSelectThreads / 64) + 1];
     __shared__ int picked[3];
     const int tid = threadIdx.x, i = blockIdx.x;
     const int64_t b = blockIdx.y;
@@ -280,33 +316,72 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
     const int64_t row = b * p.n_sel + i;
     const int32_t *table = p.block_table + b * p.max_blocks_per_seq;
     int32_t *out = p.tiles + row * want;
-    auto tile = [&](int page) { return (int32_t)(table[page] * p.tile_block + g * p.tile_head); };
+    auto tile = [&](int block) { return (int32_t)(block * p.tile_block + g * p.tile_head); };
     if (i == 0 && tid == 0) p.sel_lens[b] = pages <= want ? L : L - kBlockTokens * (pages - want);
     if (pages <= want) {
-        for (int k = tid; k < want; k += kSelectThreads) out[k] = k < pages ? tile(k) : -1;
+        for (int k = tid; k < want; k += kSelectThreads) out[k] = k < pages ? tile(table[k]) : -1;
         return;
     }
     const unsigned *keys = p.keys + row * p.max_blocks_per_seq;
-    unsigned least = 0, mask = 0;                                  // the smallest taken key's leading bits
-    int left = want, equal = 0;                                    // wanted of the keys that share them, how many do
-    for (int pass = 0; left != equal && pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-        const unsigned digits = pass == 2 ? 1023 : 2047;
-        for (int k = tid; k < kSelectBins; k += kSelectThreads) hist[k] = 0;
-        __syncthreads();
-        for (int k0 = 0; k0 < pages; k0 += 4 * kSelectThreads) {
-            unsigned key[4];
+    unsigned key[KEYS];
+    int id[KEYS];                                                  // their blocks, on the way at the same time
+    int from = 0;                                                  // page of key e: from + e kSelectThreads
+    auto load = [&](int window) {
+        from = window * WINDOW + tid;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) key[e] = keys[min(k0 + e * kSelectThreads + tid, pages - 1)];
+        for (int e = 0; e < KEYS; ++e) {
+            const int page = min(from + e * kSelectThreads, pages - 1);
+            key[e] = keys[page];
+            id[e] = table[page];
+        }
+    };
+    const int windows = ONE ? 1 : (pages + WINDOW - 1) / WINDOW;
+    if constexpr (ONE) load(0);
+    // pages that are taken in any case have the largest key, and stand apart from the range of the others
+    const int always = p.n_sink + p.n_recent;
+    unsigned low = 0xffffffffu, high = 0;
+    for (int w = 0; w < windows; ++w) {
+        if constexpr (!ONE) load(w);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (k0 + e * kSelectThreads + tid < pages && (key[e] & mask) == least) {
+        for (int e = 0; e < KEYS; ++e) {
+            low = min(low, key[e]);
+            if (key[e] != kSelectAlways) high = max(high, key[e]);
+        }
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        low = min(low, (unsigned)__shfl_xor((int)low, o));
+        high = max(high, (unsigned)__shfl_xor((int)high, o));
+    }
+    if (tid % 64 == 0) sums[tid / 64] = (unsigned long long)high << 32 | low;
+    for (int k = tid; k < kSelectBins; k += kSelectThreads) hist[k] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kSelectThreads / 64; ++w) {
+        low = min(low, (unsigned)sums[w]);
+        high = max(high, (unsigned)(sums[w] >> 32));
+    }
+    int shift = max(32 - __clz((int)(high - low | 1u)), 0);        // bits that the keys' differences have
+    unsigned least = 0;                                            // (key - low) >> shift of the smallest taken key
+    int left = want - always, equal = left == 0 ? 0 : pages - always;   // wanted of the keys that share it, how many do
+    auto rank = [&](unsigned k) { return shift < 32 ? (k - low) >> shift : 0u; };
+    while (left != equal && left > 0 && shift > 0) {
+        const unsigned before = least;
+        const int was = shift;
+        shift = max(shift - 11, 0);
+        const int bits = was - shift;
+        for (int w = 0; w < windows; ++w) {
+            if constexpr (!ONE) load(w);
+#pragma unroll
+            for (int e = 0; e < KEYS; ++e) {
+                const unsigned r = rank(key[e]);
+                if (from + e * kSelectThreads < pages && key[e] != kSelectAlways && (was < 32 ? r >> bits : 0u) == before) {
                     // (lanes that share a digit with their wave's first are counted by one of them)
-                    const int d = key[e] >> shift & digits, d0 = __builtin_amdgcn_readfirstlane(d);
+                    const int d = (int)(r & ((1u << bits) - 1)), d0 = __builtin_amdgcn_readfirstlane(d);
                     const unsigned long long same = __ballot(d == d0);
                     if (d != d0) atomicAdd(&hist[d], 1);
-                    else if (__builtin_amdgcn_mbcnt_hi((unsigned)(same >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)same, 0)) == 0)
-                        atomicAdd(&hist[d0], __popcll(same));
+                    else if (lanes_below(same) == 0)
+                        atomicAdd(&hist[d0], (int)__popcll(same));
                 }
             }
         }
@@ -331,29 +406,62 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
                 above += c[e];
             }
         }
+        for (int k = tid; k < kSelectBins; k += kSelectThreads) hist[k] = 0;
         __syncthreads();
-        least |= (unsigned)picked[0] << shift;
-        mask |= digits << shift;
+        least = before << bits | (unsigned)picked[0];
         left = picked[1];
         equal = picked[2];
         __syncthreads();
     }
-    // a run of neighbouring pages a thread
-    const int run = (pages + kSelectThreads - 1) / kSelectThreads, from = min(tid * run, pages), to = min(from + run, pages);
-    unsigned above = 0, same = 0;
-    for (int k = from; k < to; ++k) {
-        const unsigned key = keys[k] & mask;
-        above += key > least;
-        same += key == least;
-    }
-    unsigned long long all;
-    const unsigned long long before = threads_before((unsigned long long)above << 32 | same, sums, &all);
-    int same_before = (int)(unsigned)before, at = (int)(before >> 32) + min(same_before, left);
-    for (int k = from; k < to; ++k) {
-        const unsigned key = keys[k] & mask;
-        const bool equals = key == least;
-        if (key > least || (equals && same_before < left)) out[at++] = tile(k);
-        same_before += equals;
+    // (where all that share the last digits are wanted, or none, the pass that would tell them apart is left out)
+    int taken = 0, same_taken = 0;                                 // of the windows before
+    for (int w = 0; w < windows; ++w) {
+        if constexpr (!ONE) load(w);
+        auto kind = [&](int e) {                                   // 2 taken, 1 one of the equal ones, 0 not
+            if (from + e * kSelectThreads >= pages) return 0;
+            if (key[e] == kSelectAlways) return 2;
+            const unsigned r = rank(key[e]);
+            return r > least ? 2 : r == least ? 1 : 0;
+        };
+        // counts of each wave's 64 pages, then what lies before them
+        constexpr int WAVES = kSelectThreads / 64, ENTRIES = KEYS * WAVES, EACH = (ENTRIES + 63) / 64;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < KEYS; ++e) {
+            const unsigned long long m2 = __ballot(kind(e) == 2), m1 = __ballot(kind(e) == 1);
+            if (tid % 64 == 0) counts[e * WAVES + tid / 64] = (unsigned long long)__popcll(m2) << 32 | (unsigned)__popcll(m1);
+        }
+        __syncthreads();
+        if (tid < 64) {
+            unsigned long long c[EACH], sum = 0;
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                c[k] = sum;
+                if (tid * EACH + k < ENTRIES) sum += counts[tid * EACH + k];
+            }
+            unsigned long long upto = sum;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const unsigned long long x = __shfl_up(upto, o);
+                upto += tid >= o ? x : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < EACH; ++k)
+                if (tid * EACH + k < ENTRIES) counts[tid * EACH + k] = c[k] + upto - sum;
+            if (tid == 63) counts[ENTRIES] = upto;
+        }
+        __syncthreads();
+        const unsigned long long all = counts[ENTRIES];
+#pragma unroll
+        for (int e = 0; e < KEYS; ++e) {
+            const int is = kind(e);
+            const unsigned long long m2 = __ballot(is == 2), m1 = __ballot(is == 1), before = counts[e * WAVES + tid / 64];
+            const int same_before = same_taken + (int)(unsigned)before + lanes_below(m1);
+            const int at = taken + (int)(before >> 32) + lanes_below(m2) + min(same_before, left) - min(same_taken, left);
+            if (is == 2 || (is == 1 && same_before < left)) out[at] = tile(id[e]);
+        }
+        taken += (int)(all >> 32) + min(same_taken + (int)(unsigned)all, left) - min(same_taken, left);
+        same_taken += (int)(unsigned)all;
     }
 }
 

@@ -11,6 +11,8 @@
 
 namespace hetis {
 
+constexpr int kRopeMostRows = 65535 * kRopeRows;     // of a token
+
 static int check_rope(const hetis_rope *r, int32_t head_dim)
 {
     if (!r) return HETIS_ERR_NULL;
@@ -22,14 +24,16 @@ static int check_rope(const hetis_rope *r, int32_t head_dim)
 }
 
 template <int D, bool STORE>
-static int launch_rope_u(const RopeParams &p, hipStream_t st)
+static int launch_rope_u(RopeParams p, hipStream_t st)
 {
-    // Four rows of a thread on their way where that leaves enough workgroups, one otherwise.
+    // Four rows of a thread on their way where that leaves enough workgroups, one otherwise; the rows of a token in as few
+    // workgroups as hold them, and in equal shares.
     const int64_t tokens = ((int64_t)p.n_tokens + kRopeTokens<D> - 1) / kRopeTokens<D>;
-    auto groups = [&](int u) { return ((int64_t)p.rows + kRopeRows * u - 1) / (kRopeRows * u); };
+    auto groups = [&](int u) { return (p.rows + kRopeRows * u - 1) / (kRopeRows * u); };
     const bool many = tokens * groups(4) >= 2048;
-    const dim3 grid((unsigned)std::min<int64_t>(tokens, (int64_t)1 << 23),
-                    (unsigned)std::min<int64_t>(groups(many ? 4 : 1), 65535));
+    const int n = groups(many ? 4 : 1);
+    p.rows_of_wg = ((p.rows + n - 1) / n + kRopeRows - 1) / kRopeRows * kRopeRows;
+    const dim3 grid((unsigned)std::min<int64_t>(tokens, (int64_t)1 << 23), (unsigned)n);
     return many ? launch_kv(rope_kernel<D, STORE, 4>, grid, st, p) : launch_kv(rope_kernel<D, STORE, 1>, grid, st, p);
 }
 
@@ -53,7 +57,8 @@ static int store_call(const hetis_attn_shape *shape, const hetis_rope *rope, con
     if (!token_seq && n_tokens > shape->batch) return HETIS_ERR_BAD_SHAPE;
     const int group = shape->n_q_heads / shape->n_kv_heads;
     const int64_t rows = (int64_t)n_sel * (2 + (q ? group : 0));
-    if (rows > 0x7fffffff) return HETIS_ERR_UNSUPPORTED;
+    // (a grid's limit, and that of a division by multiplication)
+    if (rows > kRopeMostRows || rows * (2 + group) > 0xffffffffLL) return HETIS_ERR_UNSUPPORTED;
     if (!inv_freq || !k_new || !v_new || !token_pos || !angle_pos || !block_table || !head_ids || !k_cache || !v_cache)
         return HETIS_ERR_NULL;
     if ((q == nullptr) != (q_out == nullptr)) return HETIS_ERR_NULL;
@@ -81,6 +86,8 @@ static int store_call(const hetis_attn_shape *shape, const hetis_rope *rope, con
     p.num_blocks = num_blocks;
     p.n_tokens = (int32_t)n_tokens;
     p.rows = (int32_t)rows;
+    const uint32_t of_head = 2 + (q ? group : 0);
+    p.of_head_inverse = (uint32_t)((((uint64_t)1 << 32) + of_head - 1) / of_head);
     p.n_kv_heads = shape->n_kv_heads;
     p.group = group;
     p.batch = shape->batch;
@@ -132,6 +139,7 @@ int hetis_rope_rows(const hetis_rope *rope, const double *inv_freq, const void *
     if (out_stride_token == 0) out_stride_token = row;
     if (stride_token < row || out_stride_token < row || stride_token % 8 != 0 || out_stride_token % 8 != 0)
         return HETIS_ERR_BAD_SHAPE;
+    if (n_heads > kRopeMostRows) return HETIS_ERR_UNSUPPORTED;
     if (!inv_freq || !rows || !positions || !out) return HETIS_ERR_NULL;
     if (out == rows && out_stride_token != stride_token) return HETIS_ERR_BAD_SHAPE;
     if (n_tokens == 0) return HETIS_OK;

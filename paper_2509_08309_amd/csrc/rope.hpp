@@ -27,7 +27,8 @@ struct RopeParams {
     int64_t stride_q, stride_q_out;         // elements between tokens
     int64_t stride_block, stride_head;      // elements
     int64_t num_blocks;
-    int32_t n_tokens, rows;                 // rows of a token
+    int32_t n_tokens, rows, rows_of_wg;     // rows of a token, and those of a workgroup
+    uint32_t of_head_inverse;               // ceil(2^32 / rows of a selected head)
     int32_t n_kv_heads, group, batch, max_blocks_per_seq, slot_bias, angle_bias;
     int32_t rot_dim, interleaved;
     float magnitude, eps;
@@ -63,7 +64,7 @@ __device__ __forceinline__ void rope_row(float (&x)[16], bool norm, const f16x8_
         sum += dpp_mov<0xB1>(sum);                      // the D / 16 lanes of a row: 4, or 8
         sum += dpp_mov<0x4E>(sum);
         if (D == 128) sum += dpp_mov<0x141>(sum);
-        const float inv = 1.f / sqrtf(sum * (1.f / D) + eps);
+        const float inv = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, 1.f / D, eps));    // (a unit in the last place off)
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = x[e] * inv * (float)w[e / 8][e % 8];
     }
@@ -86,7 +87,8 @@ __device__ __forceinline__ void rope_row(float (&x)[16], bool norm, const f16x8_
 }
 
 // STORE: rows of a token are, selected head by selected head, its query rows, the key row, the value row.
-// Otherwise they are the heads of a token.  U: rows that a thread has on their way at a time.
+// Otherwise they are the heads of a token.  U: rows that a thread has on their way at a time; they are asked for ahead of
+// everything else, so that angles and slots are worked out while they come.
 template <int D, bool STORE, int U>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeParams p)
 {
@@ -100,19 +102,54 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeParams p)
     // dims of the two pieces
     const int d0 = !p.interleaved && rotates ? 8 * l : 16 * l;
     const int d1 = !p.interleaved && rotates ? 8 * l + rot / 2 : 16 * l + 8;
+    const int queries = STORE && p.q ? p.group : 0;
+    const int r0 = blockIdx.y * p.rows_of_wg;
+    const int r1 = min(r0 + p.rows_of_wg, p.rows);
     for (int64_t n0 = (int64_t)blockIdx.x * T; n0 < p.n_tokens; n0 += (int64_t)gridDim.x * T) {
-        {
-            const int64_t n = n0 + tid / (D / 2);
-            const int i = tid % (D / 2);
-            if (n < p.n_tokens && i < rot / 2) {
-                const float2 t = rope_turn((double)p.positions[n] + p.angle_bias, p.inv_freq[i]);
-                cs[0][tid / (D / 2)][i] = t.x * p.magnitude;
-                cs[1][tid / (D / 2)][i] = t.y * p.magnitude;
-            }
-        }
         const int64_t n = n0 + tok;
         bool live = n < p.n_tokens;
-        int64_t in_tile = 0, block = 0;                 // element of the slot's row in its tile, block
+        int64_t in_tile = 0, block = 0;                 // element of the slot's row of head 0, block
+        float c[8], s[8];
+        const __half *q = p.q + n * p.stride_q, *k = p.k + n * p.n_kv_heads * D, *v = p.v + n * p.n_kv_heads * D;
+        int head[U], kind[U];                           // kind: 0 query, 1 key, 2 value, 3 nothing
+        unsigned at[U];                                 // element of its source, in its token
+        f16x8_t a[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = r0 + u * kRopeRows + slot;
+            kind[u] = 3;
+            head[u] = 0;
+            at[u] = 0;
+            if (n >= p.n_tokens || i >= r1) continue;
+            if (!STORE) {
+                kind[u] = 0;
+                at[u] = (unsigned)i * D;
+                continue;
+            }
+            const int j = (int)__umulhi((unsigned)i, p.of_head_inverse), w = i - j * (queries + 2), g = p.head_ids[j];
+            if (g < 0 || g >= p.n_kv_heads) continue;
+            kind[u] = w < queries ? 0 : w == queries ? 1 : 2;
+            head[u] = g;
+            at[u] = (unsigned)(w < queries ? g * p.group + w : g) * D;
+            // (in place a row that is named twice would be rotated twice)
+            if (kind[u] == 0 && p.q == p.q_out)
+                for (int m = 0; m < j; ++m)
+                    if (p.head_ids[m] == g) kind[u] = 3;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (kind[u] != 3) {
+                const __half *from = (kind[u] == 0 ? q : kind[u] == 1 ? k : v) + at[u];
+                a[u][0] = __builtin_nontemporal_load(reinterpret_cast<const f16x8_t *>(from + d0));
+                a[u][1] = __builtin_nontemporal_load(reinterpret_cast<const f16x8_t *>(from + d1));
+            }
+        const int64_t m = n0 + tid / (D / 2);
+        const int pair = tid % (D / 2);
+        if (m < p.n_tokens && pair < rot / 2) {
+            const float2 t = rope_turn((double)p.positions[m] + p.angle_bias, p.inv_freq[pair]);
+            cs[0][tid / (D / 2)][pair] = t.x * p.magnitude;
+            cs[1][tid / (D / 2)][pair] = t.y * p.magnitude;
+        }
         if (STORE && live) {
             const int64_t b = p.token_seq ? (int64_t)p.token_seq[n] : n;
             const int64_t pos = (int64_t)p.token_pos[n] + p.slot_bias, j = pos / kBlockTokens;
@@ -120,11 +157,10 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeParams p)
             if (live) {
                 block = p.block_table[b * p.max_blocks_per_seq + j];
                 live = block >= 0 && block < p.num_blocks;
-                in_tile = pos % kBlockTokens * D;
+                in_tile = block * p.stride_block + pos % kBlockTokens * D;
             }
         }
         __syncthreads();
-        float c[8], s[8];
         if (rotates) {
 #pragma unroll
             for (int e = 0; e < 8; e += 4) {
@@ -132,68 +168,32 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeParams p)
                 *reinterpret_cast<float4 *>(s + e) = *reinterpret_cast<const float4 *>(&cs[1][tok][8 * l + e]);
             }
         }
-        for (int r0 = blockIdx.y * (kRopeRows * U); r0 < p.rows; r0 += gridDim.y * (kRopeRows * U)) {
-            const __half *from[U];
-            __half *to[U];
-            int kind[U];                                // 0 query, 1 key, 2 value, 3 nothing
+        __half *q_out = p.q_out + n * p.stride_q_out;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int row = r0 + u * kRopeRows + slot;
-                kind[u] = 3;
-                from[u] = nullptr;
-                to[u] = nullptr;
-                if (!live || row >= p.rows) continue;
-                if (!STORE) {
-                    kind[u] = 0;
-                    from[u] = p.q + n * p.stride_q + (int64_t)row * D;
-                    to[u] = p.q_out + n * p.stride_q_out + (int64_t)row * D;
-                    continue;
+        for (int u = 0; u < U; ++u) {
+            if (kind[u] == 3 || !live) continue;
+            if (kind[u] < 2) {
+                const __half *weight = kind[u] == 0 ? p.q_weight : p.k_weight;
+                f16x8_t w[2] = {};
+                if (weight) {
+                    w[0] = *reinterpret_cast<const f16x8_t *>(weight + d0);
+                    w[1] = *reinterpret_cast<const f16x8_t *>(weight + d1);
                 }
-                const int queries = p.q ? p.group : 0;
-                const int j = row / (queries + 2), w = row % (queries + 2), g = p.head_ids[j];
-                if (g < 0 || g >= p.n_kv_heads) continue;
-                if (w < queries) {
-                    const int64_t h = (int64_t)g * p.group + w;
-                    kind[u] = 0;
-                    // (in place a row that is named twice would be rotated twice)
-                    if (p.q == p.q_out)
-                        for (int i = 0; i < j; ++i)
-                            if (p.head_ids[i] == g) kind[u] = 3;
-                    from[u] = p.q + n * p.stride_q + h * D;
-                    to[u] = p.q_out + n * p.stride_q_out + h * D;
-                } else {
-                    kind[u] = w == queries ? 1 : 2;
-                    from[u] = (kind[u] == 1 ? p.k : p.v) + (n * p.n_kv_heads + g) * D;
-                    to[u] = (kind[u] == 1 ? p.k_cache : p.v_cache) + block * p.stride_block + g * p.stride_head + in_tile;
-                }
+                float x[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = (float)a[u][e / 8][e % 8];
+                rope_row<D>(x, weight != nullptr, w, p.eps, rotates, p.interleaved, c, s);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) a[u][e / 8][e % 8] = (_Float16)x[e];
             }
-            f16x8_t a[U][2];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (kind[u] != 3) {
-                    a[u][0] = __builtin_nontemporal_load(reinterpret_cast<const f16x8_t *>(from[u] + d0));
-                    a[u][1] = __builtin_nontemporal_load(reinterpret_cast<const f16x8_t *>(from[u] + d1));
-                }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (kind[u] < 2) {
-                    const __half *weight = kind[u] == 0 ? p.q_weight : p.k_weight;
-                    f16x8_t w[2] = {};
-                    if (weight) {
-                        w[0] = *reinterpret_cast<const f16x8_t *>(weight + d0);
-                        w[1] = *reinterpret_cast<const f16x8_t *>(weight + d1);
-                    }
-                    float x[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) x[e] = (float)a[u][e / 8][e % 8];
-                    rope_row<D>(x, weight != nullptr, w, p.eps, rotates, p.interleaved, c, s);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) a[u][e / 8][e % 8] = (_Float16)x[e];
-                }
-                if (kind[u] != 3) {
-                    *reinterpret_cast<f16x8_t *>(to[u] + d0) = a[u][0];
-                    *reinterpret_cast<f16x8_t *>(to[u] + d1) = a[u][1];
-                }
+            __half *to = kind[u] == 0 ? q_out + at[u] : (kind[u] == 1 ? p.k_cache : p.v_cache) + in_tile + head[u] * p.stride_head;
+            // (many rows are more than the caches hold; a few are about to be read)
+            if (U > 1) {
+                __builtin_nontemporal_store(a[u][0], reinterpret_cast<f16x8_t *>(to + d0));
+                __builtin_nontemporal_store(a[u][1], reinterpret_cast<f16x8_t *>(to + d1));
+            } else {
+                *reinterpret_cast<f16x8_t *>(to + d0) = a[u][0];
+                *reinterpret_cast<f16x8_t *>(to + d1) = a[u][1];
             }
         }
         __syncthreads();                                // (the next tokens' turns)

@@ -51,17 +51,28 @@ constexpr int kPfWaves = 4;
 constexpr int kPfThreads = 64 * kPfWaves;
 constexpr int kPfRows = 32 * kPfWaves;      // rows of a tile
 constexpr int kPfStep = 64;                 // cached tokens of a step
-// A sequence of few tiles over a long cache is cut along the cache as well, by its own numbers only: into at most
-// kPfSplitItems / tiles segments of at least kPfSegSteps steps.
-constexpr int kPfSplitTiles = 8, kPfSplitItems = 32, kPfSegSteps = 16;
+// A sequence's first tiles, up to kPfSplitTiles of them, are cut along the cache as well, by the sequence's own numbers
+// only: into at most kPfSplitItems / tiles segments of at least kPfSegSteps steps.  All tiles of a few drafted tokens
+// over a long cache, and of a long chunk those that come last: without them its tiles, all about as long, leave most of
+// the chip idle in their last round.
+constexpr int kPfSplitTiles = 8, kPfSplitItems = 32, kPfSegSteps = 16, kPfSegStepsOfMany = 48;
 constexpr int kPfQueues = 8;
 constexpr int kPfBatch = 8;                 // segments that are added up at a time
 enum : int { kPfCtlTickets = 16, kPfCtlGone = 24 };      // control words: a queue's tickets, workgroups finished
 
 // What there is to do for a sequence.
 struct PrefillSequence {
-    int b, start, fresh, len, rows, tiles, segs, seg_steps; // rows: tokens with a row; seg_steps: steps of a segment
-    __device__ __forceinline__ int items() const { return tiles * segs; }
+    int b, start, fresh, len, rows, tiles;  // rows: tokens with a row
+    int cut, segs, seg_steps;               // the first `cut` tiles are `segs` items each, of up to seg_steps steps
+    int longest;                            // steps of an item
+    __device__ __forceinline__ int items() const { return tiles + cut * (segs - 1); }
+    // item u, by ascending positions: its tile and segment
+    __device__ __forceinline__ int item(int u, int *seg) const
+    {
+        const int v = u - cut * segs, tile = v < 0 ? (int)((unsigned)u / (unsigned)segs) : cut + v;
+        *seg = v < 0 ? u - tile * segs : 0;
+        return tile;
+    }
 };
 __device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillParams &p, int b)
 {
@@ -72,15 +83,22 @@ __device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillParams 
     s.len = p.seq_lens[b];
     // (rows that q does not have are no work)
     s.rows = s.start < 0 || s.start >= p.n_tokens ? 0 : min(max(s.fresh, 0), p.n_tokens - s.start);
-    const int steps = (min(max(s.len, 0), p.max_blocks_per_seq * kBlockTokens) + kPfStep - 1) / kPfStep;
+    auto steps_of = [&](int seen) { return (min(max(seen, 0), p.max_blocks_per_seq * kBlockTokens) + kPfStep - 1) / kPfStep; };
     s.tiles = (int)((((int64_t)s.rows << p.group_shift) + kPfRows - 1) / kPfRows);
+    s.cut = 0;
     s.segs = 1;
-    s.seg_steps = max(steps, 1);
-    if (s.tiles >= 1 && s.tiles <= kPfSplitTiles) {
-        const int want = min((steps + kPfSegSteps - 1) / kPfSegSteps, kPfSplitItems / s.tiles);
+    s.seg_steps = 0;
+    s.longest = steps_of(s.len);
+    if (s.tiles >= 1) {
+        const int cut = min(s.tiles, kPfSplitTiles);
+        const int steps = steps_of(s.len - s.fresh + min(cut << (7 - p.group_shift), s.rows));     // (of the last of them)
+        const int least = cut == s.tiles ? kPfSegSteps : kPfSegStepsOfMany;
+        const int want = min((steps + least - 1) / least, kPfSplitItems / cut);
         if (want > 1) {
+            s.cut = cut;
             s.seg_steps = (steps + want - 1) / want;
             s.segs = (steps + s.seg_steps - 1) / s.seg_steps;
+            if (cut == s.tiles) s.longest = s.seg_steps;
         }
     }
     return s;
@@ -118,18 +136,20 @@ __device__ __forceinline__ i32x4 tile_descriptor(const __half *tile, int nbytes)
 template <int D>
 __device__ __forceinline__ void page_to_lds(i32x4 r, int from0, int from1, int from2, int from3, unsigned to)
 {
+    constexpr int LOAD = 64 * 16;           // bytes of a load
     if constexpr (D == 128)
         asm volatile("s_mov_b32 m0, %5\n\ts_nop 4\n\t"
                      "buffer_load_dwordx4 %0, %4, 0 offen lds\n\t"
-                     "buffer_load_dwordx4 %1, %4, 0 offen offset:1024 lds\n\t"
-                     "buffer_load_dwordx4 %2, %4, 0 offen offset:2048 lds\n\t"
-                     "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds"
-                     :: "v"(from0), "v"(from1), "v"(from2), "v"(from3), "s"(r), "s"(to) : "memory");
+                     "buffer_load_dwordx4 %1, %4, 0 offen offset:%6 lds\n\t"
+                     "buffer_load_dwordx4 %2, %4, 0 offen offset:%7 lds\n\t"
+                     "buffer_load_dwordx4 %3, %4, 0 offen offset:%8 lds"
+                     :: "v"(from0), "v"(from1), "v"(from2), "v"(from3), "s"(r), "s"(to), "n"(LOAD), "n"(2 * LOAD),
+                        "n"(3 * LOAD) : "memory");
     else
         asm volatile("s_mov_b32 m0, %3\n\ts_nop 4\n\t"
                      "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
-                     "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds"
-                     :: "v"(from0), "v"(from3), "s"(r), "s"(to) : "memory");
+                     "buffer_load_dwordx4 %1, %2, 0 offen offset:%4 lds"
+                     :: "v"(from0), "v"(from3), "s"(r), "s"(to), "n"(LOAD) : "memory");
 }
 
 // Pieces of a row change places with its number, so that the lanes that read together meet different banks: 16 rows at
@@ -187,8 +207,9 @@ __device__ __forceinline__ void prefill_store(const float (&o)[16], float l, __h
     }
 }
 
-template <int D>
-__device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<D> &sh, const PrefillItem &item)
+// `late` is called once, by all threads, when most of the item's work is done.
+template <int D, class F>
+__device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<D> &sh, const PrefillItem &item, F late)
 {
     constexpr int KS = D / 16;              // products of a score
     constexpr int DB = D / 32;              // row blocks of O^T
@@ -203,14 +224,15 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
     const PrefillSequence &seq = item.seq;
     const int start = seq.start, fresh = seq.fresh, L = seq.len;
     const int t_first = item.tile << (7 - p.group_shift);               // tokens of a tile: 128 / r
-    if (t_first >= seq.rows) return;
+    if (t_first >= seq.rows) return late();
     const int t_last = min(t_first + (kPfRows >> p.group_shift), seq.rows) - 1;
     const int seen = min(max(L - fresh + t_last + 1, 0), p.max_blocks_per_seq * kBlockTokens);
     const int pages = (seen + kBlockTokens - 1) / kBlockTokens;
     const int all_steps = (seen + kPfStep - 1) / kPfStep;
-    const int first = item.seg * seq.seg_steps, steps = min(all_steps, first + seq.seg_steps);
-    if (item.seg > 0 && first >= all_steps) return;
-    const int tile_segs = max((all_steps + seq.seg_steps - 1) / seq.seg_steps, 1);
+    const int seg_steps = item.tile < seq.cut ? seq.seg_steps : max(all_steps, 1);
+    const int first = item.seg * seg_steps, steps = min(all_steps, first + seg_steps);
+    if (item.seg > 0 && first >= all_steps) return late();
+    const int tile_segs = max((all_steps + seg_steps - 1) / seg_steps, 1);
 
     // this lane's row
     const int row = wave * 32 + n, token = t_first + (row >> p.group_shift);
@@ -295,6 +317,8 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
         block1 = table[min(page + kPfStep / kBlockTokens, pages - 1)];
         asked = ask_id(first + 2);
         bring(first, false, block0);
+        bring(first, true, block0);
+        if (first + 1 < steps) bring(first + 1, false, block1);
     }
     pf_f16x8 q[KS];
 #pragma unroll
@@ -410,8 +434,6 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
     if (first < steps) {
         drain();
         meet();
-        bring(first, true, block0);
-        if (first + 1 < steps) bring(first + 1, false, block1);
         if (first < own_steps) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -441,8 +463,11 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
     if (step < own_steps) {
         settle(step);
         turn(step);
+        late();
         attend(step, std::false_type());
         ++step;
+    } else {
+        late();
     }
     for (; step < steps; ++step) turn(step);            // (the other waves' rows lie further on)
     drain();
@@ -574,7 +599,7 @@ struct PrefillQueues {
             int key = -1;
             if (tid < p.batch) {
                 s = prefill_sequence(p, tid);
-                key = s.seg_steps;
+                key = s.longest;
             }
             sh.key[tid] = key;
             __syncthreads();
@@ -588,20 +613,24 @@ struct PrefillQueues {
             if (tid < p.batch) sh.sequences[rank] = s;
             __syncthreads();
         }
-        // items of every queue
-        int total[kPfQueues] = {};
+    }
+    // Items of every queue (needed by workgroups that have nothing left in theirs).
+    __device__ __forceinline__ void count()
+    {
+        const int tid = thread_here();
+        int all[kPfQueues] = {};
         each([&](int rank, int items) {
             int h0;
 #pragma unroll
-            for (int y = 0; y < kPfQueues; ++y) total[y] += items * pairs_in(y, rank, &h0);
+            for (int y = 0; y < kPfQueues; ++y) all[y] += items * pairs_in(y, rank, &h0);
         });
 #pragma unroll
         for (int o = 32; o; o >>= 1)
 #pragma unroll
-            for (int y = 0; y < kPfQueues; ++y) total[y] += __shfl_xor(total[y], o);
+            for (int y = 0; y < kPfQueues; ++y) all[y] += __shfl_xor(all[y], o);
 #pragma unroll
         for (int y = 0; y < kPfQueues; ++y)
-            if (tid % 64 == y) sh.totals[tid / 64][y] = total[y];
+            if (tid % 64 == y) sh.totals[tid / 64][y] = all[y];
         __syncthreads();
     }
     // f(rank, items of a head) for this thread's sequences
@@ -622,8 +651,8 @@ struct PrefillQueues {
         for (int w = 0; w < kPfWaves; ++w) t += sh.totals[w][queue];
         return t;
     }
-    // items of the queue ahead of each thread's
-    __device__ __forceinline__ void open(int queue)
+    // items of the queue ahead of each thread's; returns how many there are
+    __device__ __forceinline__ int open(int queue)
     {
         const int tid = thread_here(), lane = tid % 64, wave = tid / 64;
         int sum = 0, h0;
@@ -641,6 +670,7 @@ struct PrefillQueues {
         sh.before[tid + 1] = upto;
         if (tid == 0) sh.before[0] = 0;
         __syncthreads();
+        return __builtin_amdgcn_readfirstlane(sh.before[kPfThreads]);
     }
     // Item k of the open queue: of a sequence the tiles that see most first, one for each head.
     __device__ __forceinline__ PrefillItem find(int queue, int k)
@@ -652,10 +682,9 @@ struct PrefillQueues {
                 const PrefillSequence s = per == 1 ? sh.sequences[rank] : prefill_sequence(p, rank);
                 const int pairs = pairs_in(queue, rank, &h0), items = s.items() * pairs;
                 if (rem < items) {
-                    const unsigned u = (unsigned)rem / (unsigned)pairs, tile = u / (unsigned)s.segs;
-                    sh.item.head = h0 + kPfQueues * (rem - (int)u * pairs);
-                    sh.item.tile = s.tiles - 1 - (int)tile;
-                    sh.item.seg = (int)(u - tile * s.segs);
+                    const int u = (int)((unsigned)rem / (unsigned)pairs);
+                    sh.item.head = h0 + kPfQueues * (rem - u * pairs);
+                    sh.item.tile = s.item(s.items() - 1 - u, &sh.item.seg);
                     sh.item.seq = s;
                     break;
                 }
@@ -694,8 +723,7 @@ __device__ __forceinline__ PrefillItem prefill_direct(const PrefillParams &p, in
     item.head = number % p.n_sel;
     item.seq = prefill_sequence(p, __builtin_amdgcn_readfirstlane(lo));
     const int u = place - (max(item.seq.start, 0) >> token_shift) - item.seq.b * p.gap;
-    item.tile = u < 0 ? -1 : u / item.seq.segs;
-    item.seg = u < 0 ? 0 : u % item.seq.segs;
+    item.tile = u < 0 ? -1 : item.seq.item(u, &item.seg);
     return item;
 }
 
@@ -704,7 +732,7 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_direct_kernel(PrefillPa
 {
     __shared__ __attribute__((aligned(16))) PrefillLds<D> sh;
     const PrefillItem item = prefill_direct(p, blockIdx.x);
-    if (item.tile >= 0) prefill_item<D>(p, sh, item);
+    if (item.tile >= 0) prefill_item<D>(p, sh, item, [] {});
 }
 
 template <int D>
@@ -714,22 +742,23 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_kernel(PrefillParams p)
     PrefillQueues<D> queues(p, sh);
     const int tid = threadIdx.x, places = gridDim.x / kPfQueues;        // workgroups of a queue
     int queue = blockIdx.x % kPfQueues, k = blockIdx.x / kPfQueues, tried = 0;
-    queues.open(queue);
+    int total = queues.open(queue);
     for (;;) {
-        const int total = queues.total(queue);
         if (k < total) {
             const PrefillItem item = queues.find(queue, k);
-            // the next ticket is on its way meanwhile
+            // The next ticket is drawn late, so that no workgroup sits on an item while another has none.
             unsigned next = 0;
-            if (tid == 0 && total > places)
-                next = __hip_atomic_fetch_add(p.control + kPfCtlTickets + queue, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            prefill_item<D>(p, sh, item);
+            prefill_item<D>(p, sh, item, [&] {
+                if (tid == 0 && total > places)
+                    next = __hip_atomic_fetch_add(p.control + kPfCtlTickets + queue, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            });
             if (tid == 0) sh.ticket = total > places ? places + (int)next : total;
             meet_lds();                                 // (the item's results may still be on their way out)
             k = __builtin_amdgcn_readfirstlane(sh.ticket);
             continue;
         }
         // the others: only those with more items than workgroups that start on them
+        if (tried == 0) queues.count();
         do {
             queue = (queue + 1) % kPfQueues;
             ++tried;
@@ -740,7 +769,8 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_kernel(PrefillParams p)
             sh.ticket = places + (int)__hip_atomic_fetch_add(p.control + kPfCtlTickets + queue, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         k = sh.ticket;
-        if (k < queues.total(queue)) queues.open(queue);
+        total = queues.total(queue);
+        if (k < total) queues.open(queue);
     }
     // the last workgroup to leave puts the tickets back
     if (tid == 0) {

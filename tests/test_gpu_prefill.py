@@ -131,6 +131,52 @@ def test_many_sequences(hq, hkv, D):
     c.check(c.run([hkv - 1]), [hkv - 1], sequences=np.r_[0:4500:37, 64, 4095, 4096, 4499], every=7)
 
 
+@pytest.mark.parametrize("D,hq,hkv,lens,new", [
+    (64, 8, 1, [7000, 30], [147, 2]), (128, 8, 1, [6600], [129]), (128, 2, 2, [7500, 7400], [1025, 1160])])
+def test_chunks_whose_first_tiles_are_cut(D, hq, hkv, lens, new):
+    """More than eight tiles behind a long context: the first eight in pieces, the others whole."""
+    c = Case(lens, new, hq, hkv, D, seed=71)
+    c.check(c.run([0]), [0], every=13 if hkv == 1 else 61)
+
+
+def crowd(n, long, seed):
+    """Lengths and new tokens of n sequences, a few of them long."""
+    rng = np.random.default_rng(seed)
+    lens = rng.integers(1, 60, n)
+    new = np.minimum(rng.integers(0, 4, n), lens)
+    for b, (length, fresh) in long.items():
+        lens[b], new[b] = length, fresh
+    return lens, new
+
+
+LONG = {0: (2600, 3), 7: (6700, 150), 11: (3100, 20), 19: (300, 300), 21: (2500, 1), 22: (4000, 0)}
+
+
+@pytest.mark.parametrize("n", [23, 256, 300, 700])
+@pytest.mark.parametrize("hq,hkv,D", [(8, 1, 64), (16, 2, 128), (3, 3, 64)])
+def test_crowds_with_long_contexts(n, hq, hkv, D):
+    """Queues of pieces and whole tiles: sequences ordered by their lengths (256 and less), or as they come."""
+    lens, new = crowd(n, {(b if b < 20 else n - 23 + b): x for b, x in LONG.items()}, seed=72 + n)
+    c = Case(lens, new, hq, hkv, D, seed=73)
+    heads = list(range(hkv))
+    out = c.run(heads)
+    c.check(out, heads, sequences=np.r_[0:n:max(n // 12, 1), 7, 11, n - 2, n - 1], every=17)
+    assert np.array_equal(bits(c.run(heads)), bits(out))
+
+
+def test_a_crowd_and_its_sequences_alone():
+    """With queues and without them: the same bits."""
+    lens, new = crowd(23, LONG, seed=74)
+    c = Case(lens, new, 16, 2, 128, seed=75)
+    both = bits(c.run([0, 1]))
+    for b in (0, 7, 11, 19, 21):
+        s = slice(c.starts[b], c.starts[b + 1])
+        p, one = c.p, Case([1], [1], 16, 2, 128, seed=1)
+        one.p.lens, one.p.table, one.p.mb, one.p.k, one.p.v = p.lens[b:b + 1], p.table[b:b + 1], p.mb, p.k, p.v
+        one.new, one.starts, one.n, one.q = c.new[b:b + 1], np.array([0, new[b]]), int(new[b]), c.q[s]
+        assert np.array_equal(bits(one.run([0, 1])), both[s]), b
+
+
 def test_heads_of_a_subset_are_the_bits_of_all_heads():
     for hq, hkv, D, lens, new in ((8, 8, 64, [700, 33, 4500, 1], [700, 5, 40, 1]), (32, 4, 128, [5000, 260, 9000], [3, 260, 130])):
         c = Case(lens, new, hq, hkv, D, seed=21)

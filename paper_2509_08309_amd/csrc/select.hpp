@@ -185,6 +185,13 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(SelectParams p)
     const int first = blockIdx.y * kScorePages;
     if (pages <= p.n_pages || first >= pages) return;              // (all of them: nothing to score)
     const int g = p.head_ids[i];
+    // the head's row is asked for first: loads are waited for in the order in which they went out
+    u32x4 row[DIMS / 8];
+    {
+        const __half *from = p.q + ((b * p.n_q_heads + (int64_t)g * p.group + min(n, p.group - 1)) * D);
+#pragma unroll
+        for (int e = 0; e < DIMS / 8; ++e) row[e] = *reinterpret_cast<const u32x4 *>(from + e / 2 * 64 + quarter * 16 + e % 2 * 8);
+    }
     // the wave's pages: one id a lane, then all their codes
     const int at = first + wave * 64;
     const int mine = p.block_table[b * p.max_blocks_per_seq + min(at + lane, pages - 1)];
@@ -204,15 +211,13 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(SelectParams p)
     bool counts = n < p.group;
     i32x4 query[STEPS];
     {
-        const __half *row = p.q + ((b * p.n_q_heads + (int64_t)g * p.group + min(n, p.group - 1)) * D);
         unsigned raw[DIMS / 2], most = 0;
 #pragma unroll
         for (int e = 0; e < DIMS / 8; ++e) {
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(row + e / 2 * 64 + quarter * 16 + e % 2 * 8);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                raw[4 * e + w] = v[w];
-                most = max(most, max(v[w] & 0x7fffu, v[w] >> 16 & 0x7fffu));
+                raw[4 * e + w] = row[e][w];
+                most = max(most, max(row[e][w] & 0x7fffu, row[e][w] >> 16 & 0x7fffu));
             }
         }
         uint2 o = lanes_xor<16>(most);
@@ -241,13 +246,13 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(SelectParams p)
         for (int s = 0; s < STEPS; ++s)
             query[s] = *reinterpret_cast<const i32x4 *>(&shared[s / (STEPS / 2)][lane][s % (STEPS / 2) * 4]);
     }
-    unsigned *keys = p.keys + (b * p.n_sel + i) * p.max_blocks_per_seq;
+    float top = 0.f;                                               // of page 16 (n / 4) + 4 quarter + n % 4
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         i32x4 acc = {0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(code[k][s], query[s], acc, 0, 0, 0);
-        // lane (n, quarter): head n, pages at + 16 k + 4 quarter + e
+        // lane (n, quarter): head n, pages 16 k + 4 quarter + e
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float best = counts ? (float)acc[e] * t : -INFINITY;
@@ -255,13 +260,13 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(SelectParams p)
             best = fmaxf(best, dpp_mov<0x4E>(best));
             best = fmaxf(best, dpp_mov<0x141>(best));
             best = fmaxf(best, dpp_mov<0x140>(best));
-            const int of = 16 * k + quarter * 4 + e;
-            const float s = __shfl(s_mine, of);
-            const float score = s == INFINITY ? s : best == -INFINITY ? best : best * s;
-            if (n == 0 && at + of < pages)
-                keys[at + of] = at + of < p.n_sink || at + of >= pages - p.n_recent ? kSelectAlways : select_key(score);
+            top = n == 4 * k + e ? best : top;
         }
     }
+    const int of = n / 4 * 16 + quarter * 4 + n % 4;
+    const float s = __shfl(s_mine, of), score = s == INFINITY ? s : top == -INFINITY ? top : top * s;
+    unsigned *keys = p.keys + (b * p.n_sel + i) * p.max_blocks_per_seq;
+    if (at + of < pages) keys[at + of] = at + of < p.n_sink || at + of >= pages - p.n_recent ? kSelectAlways : select_key(score);
 }
 
 constexpr int kSelectThreads = 1024;
@@ -272,27 +277,30 @@ __device__ __forceinline__ int lanes_below(unsigned long long mask)
     return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
 }
 
-// Sum of x over the threads before this one; the sum of all in *total.
-__device__ __forceinline__ unsigned long long threads_before(unsigned long long x, unsigned long long *sums, unsigned long long *total)
+// Sum over the lanes up to this one: within sixteen lanes, then the sums of the sixteen before, then of the half before.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned add_dpp(unsigned x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ unsigned lanes_upto(unsigned x)
+{
+    x = add_dpp<0x111, 0xF>(x);
+    x = add_dpp<0x112, 0xF>(x);
+    x = add_dpp<0x114, 0xF>(x);
+    x = add_dpp<0x118, 0xF>(x);
+    x = add_dpp<0x142, 0xA>(x);
+    return add_dpp<0x143, 0xC>(x);
+}
+
+// Sum of x over the threads before this one.
+__device__ __forceinline__ unsigned threads_before(unsigned x, unsigned *sums)
 {
     constexpr int WAVES = kSelectThreads / 64;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    unsigned long long upto = x;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned long long y = __shfl_up(upto, o);
-        upto += lane >= o ? y : 0;
-    }
-    __syncthreads();
+    const unsigned upto = lanes_upto(x);
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
-    unsigned long long before = upto - x, all = 0;
+    unsigned before = upto - x;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        before += w < wave ? sums[w] : 0;
-        all += sums[w];
-    }
-    *total = all;
+    for (int w = 0; w < WAVES; ++w) before += w < wave ? sums[w] : 0;
     return before;
 }
 
@@ -306,8 +314,9 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
 {
     constexpr int PER = kSelectBins / kSelectThreads, WINDOW = kSelectThreads * KEYS;
     __shared__ int hist[kSelectBins];
-    __shared__ unsigned long long sums[kSelectThreads / 64];
-    __shared__ unsigned long long counts[KEYS * (kSelectThreads / 64) + 1];
+    __shared__ uint2 ranges[kSelectThreads / 64];
+    __shared__ unsigned sums[kSelectThreads / 64];
+    __shared__ uint2 counts[KEYS * (kSelectThreads / 64) + 1];     // of pages that are taken, and of equal ones
     __shared__ int picked[3];
     const int tid = threadIdx.x, i = blockIdx.x;
     const int64_t b = blockIdx.y;
@@ -348,18 +357,23 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
             if (key[e] != kSelectAlways) high = max(high, key[e]);
         }
     }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        low = min(low, (unsigned)__shfl_xor((int)low, o));
-        high = max(high, (unsigned)__shfl_xor((int)high, o));
-    }
-    if (tid % 64 == 0) sums[tid / 64] = (unsigned long long)high << 32 | low;
+    auto fold = [&](uint2 l, uint2 h) {
+        low = min(l.x, l.y);
+        high = max(h.x, h.y);
+    };
+    fold(make_uint2(low, dpp_u32<0xB1>(low)), make_uint2(high, dpp_u32<0xB1>(high)));
+    fold(make_uint2(low, dpp_u32<0x4E>(low)), make_uint2(high, dpp_u32<0x4E>(high)));
+    fold(make_uint2(low, dpp_u32<0x141>(low)), make_uint2(high, dpp_u32<0x141>(high)));
+    fold(make_uint2(low, dpp_u32<0x140>(low)), make_uint2(high, dpp_u32<0x140>(high)));
+    fold(lanes_xor<16>(low), lanes_xor<16>(high));
+    fold(lanes_xor<32>(low), lanes_xor<32>(high));
+    if (tid % 64 == 0) ranges[tid / 64] = make_uint2(low, high);
     for (int k = tid; k < kSelectBins; k += kSelectThreads) hist[k] = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kSelectThreads / 64; ++w) {
-        low = min(low, (unsigned)sums[w]);
-        high = max(high, (unsigned)(sums[w] >> 32));
+        low = min(low, ranges[w].x);
+        high = max(high, ranges[w].y);
     }
     int shift = max(32 - __clz((int)(high - low | 1u)), 0);        // bits that the keys' differences have
     unsigned least = 0;                                            // (key - low) >> shift of the smallest taken key
@@ -393,8 +407,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
             c[e] = hist[top - 1 - e];
             mine += c[e];
         }
-        unsigned long long all;
-        int above = (int)threads_before((unsigned long long)mine, sums, &all);
+        int above = (int)threads_before((unsigned)mine, sums);
         if (above < left && left <= above + mine) {
 #pragma unroll
             for (int e = 0; e < PER; ++e) {
@@ -429,39 +442,38 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
 #pragma unroll
         for (int e = 0; e < KEYS; ++e) {
             const unsigned long long m2 = __ballot(kind(e) == 2), m1 = __ballot(kind(e) == 1);
-            if (tid % 64 == 0) counts[e * WAVES + tid / 64] = (unsigned long long)__popcll(m2) << 32 | (unsigned)__popcll(m1);
+            if (tid % 64 == 0) counts[e * WAVES + tid / 64] = make_uint2((unsigned)__popcll(m2), (unsigned)__popcll(m1));
         }
         __syncthreads();
         if (tid < 64) {
-            unsigned long long c[EACH], sum = 0;
+            uint2 c[EACH], sum = make_uint2(0, 0);
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
                 c[k] = sum;
-                if (tid * EACH + k < ENTRIES) sum += counts[tid * EACH + k];
+                if (tid * EACH + k < ENTRIES) {
+                    sum.x += counts[tid * EACH + k].x;
+                    sum.y += counts[tid * EACH + k].y;
+                }
             }
-            unsigned long long upto = sum;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const unsigned long long x = __shfl_up(upto, o);
-                upto += tid >= o ? x : 0;
-            }
+            const uint2 upto = make_uint2(lanes_upto(sum.x), lanes_upto(sum.y));
 #pragma unroll
             for (int k = 0; k < EACH; ++k)
-                if (tid * EACH + k < ENTRIES) counts[tid * EACH + k] = c[k] + upto - sum;
+                if (tid * EACH + k < ENTRIES) counts[tid * EACH + k] = make_uint2(c[k].x + upto.x - sum.x, c[k].y + upto.y - sum.y);
             if (tid == 63) counts[ENTRIES] = upto;
         }
         __syncthreads();
-        const unsigned long long all = counts[ENTRIES];
+        const uint2 all = counts[ENTRIES];
 #pragma unroll
         for (int e = 0; e < KEYS; ++e) {
             const int is = kind(e);
-            const unsigned long long m2 = __ballot(is == 2), m1 = __ballot(is == 1), before = counts[e * WAVES + tid / 64];
-            const int same_before = same_taken + (int)(unsigned)before + lanes_below(m1);
-            const int at = taken + (int)(before >> 32) + lanes_below(m2) + min(same_before, left) - min(same_taken, left);
+            const unsigned long long m2 = __ballot(is == 2), m1 = __ballot(is == 1);
+            const uint2 before = counts[e * WAVES + tid / 64];
+            const int same_before = same_taken + (int)before.y + lanes_below(m1);
+            const int at = taken + (int)before.x + lanes_below(m2) + min(same_before, left) - min(same_taken, left);
             if (is == 2 || (is == 1 && same_before < left)) out[at] = tile(id[e]);
         }
-        taken += (int)(all >> 32) + min(same_taken + (int)(unsigned)all, left) - min(same_taken, left);
-        same_taken += (int)(unsigned)all;
+        taken += (int)all.x + min(same_taken + (int)all.y, left) - min(same_taken, left);
+        same_taken += (int)all.y;
     }
 }
 

@@ -1,8 +1,10 @@
 // Rotary positions (include/hetis_rope.h): rows of queries and keys normed and rotated, in memory or on the way
 // into the paged cache, value rows moved beside them.
 //
-// A lane holds 16 dims of a row: the two pieces of eight that rotate with each other (halves), or two
-// neighbouring ones (interleaved, and dims that do not rotate).  Either way its pairs are 8 l .. 8 l + 7.
+// A lane holds two pieces of eight dims of a row, such that neighbouring lanes' first pieces are neighbours, and their
+// second ones: the two that rotate with each other (halves; pairs 8 l .. 8 l + 7), or one of either half of the row
+// (interleaved; pairs 4 l .. and D / 4 + 4 l ..).  (With two neighbouring pieces a lane, loads and stores had gaps: 33500
+// tokens of 64 + 2 x 8 rows of 128, interleaved, into the cache 313 us; now 254, 5.4 TB/s.)
 #pragma once
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -13,6 +15,7 @@
 namespace hetis {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));    // (an array of floats would go to scratch memory)
 
 struct RopeParams {
     const double *inv_freq;
@@ -53,8 +56,8 @@ __device__ __forceinline__ float2 rope_turn(double position, double f)
 // One row's 16 dims in a lane -> normed and rotated.  (The copies of this code in the kernels below must give the
 // same bits.)
 template <int D>
-__device__ __forceinline__ void rope_row(float (&x)[16], bool norm, const f16x8_t (&w)[2], float eps, bool rotates,
-                                         int interleaved, const float (&c)[8], const float (&s)[8])
+__device__ __forceinline__ void rope_row(f32x16_t &x, bool norm, const f16x8_t (&w)[2], float eps,
+                                         bool rotates0, bool rotates1, int interleaved, const float (&c)[8], const float (&s)[8])
 {
 #pragma clang fp contract(off)
     if (norm) {
@@ -68,15 +71,22 @@ __device__ __forceinline__ void rope_row(float (&x)[16], bool norm, const f16x8_
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = x[e] * inv * (float)w[e / 8][e % 8];
     }
-    if (!rotates) return;
     if (interleaved) {
+        if (rotates0)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float u = x[2 * e], y = x[2 * e + 1];
-            x[2 * e] = __builtin_fmaf(u, c[e], -(y * s[e]));
-            x[2 * e + 1] = __builtin_fmaf(y, c[e], u * s[e]);
-        }
-    } else {
+            for (int e = 0; e < 4; ++e) {
+                const float u = x[2 * e], y = x[2 * e + 1];
+                x[2 * e] = __builtin_fmaf(u, c[e], -(y * s[e]));
+                x[2 * e + 1] = __builtin_fmaf(y, c[e], u * s[e]);
+            }
+        if (rotates1)
+#pragma unroll
+            for (int e = 4; e < 8; ++e) {
+                const float u = x[2 * e], y = x[2 * e + 1];
+                x[2 * e] = __builtin_fmaf(u, c[e], -(y * s[e]));
+                x[2 * e + 1] = __builtin_fmaf(y, c[e], u * s[e]);
+            }
+    } else if (rotates0) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float u = x[e], y = x[e + 8];
@@ -98,10 +108,11 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeParams p)
     __shared__ __attribute__((aligned(16))) float cs[2][T][D / 2];
     const int tid = threadIdx.x, l = tid % LR, slot = tid / LR % kRopeRows, tok = tid / (LR * kRopeRows);
     const int rot = p.rot_dim;
-    const bool rotates = l < rot / 16;
     // dims of the two pieces
-    const int d0 = !p.interleaved && rotates ? 8 * l : 16 * l;
-    const int d1 = !p.interleaved && rotates ? 8 * l + rot / 2 : 16 * l + 8;
+    const int behind = l - rot / 16;                    // of the lanes whose dims do not rotate (halves)
+    const int d0 = p.interleaved || behind < 0 ? 8 * l : rot + 8 * behind;
+    const int d1 = d0 + (p.interleaved ? D : behind < 0 ? rot : D - rot) / 2;
+    const bool rotates0 = d0 < rot, rotates1 = d1 < rot;
     const int queries = STORE && p.q ? p.group : 0;
     const int r0 = blockIdx.y * p.rows_of_wg;
     const int r1 = min(r0 + p.rows_of_wg, p.rows);
@@ -161,12 +172,11 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeParams p)
             }
         }
         __syncthreads();
-        if (rotates) {
+        const int pair0 = p.interleaved ? 4 * l : 8 * l, pair1 = pair0 + (p.interleaved ? D / 4 : 4);
 #pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                *reinterpret_cast<float4 *>(c + e) = *reinterpret_cast<const float4 *>(&cs[0][tok][8 * l + e]);
-                *reinterpret_cast<float4 *>(s + e) = *reinterpret_cast<const float4 *>(&cs[1][tok][8 * l + e]);
-            }
+        for (int e = 0; e < 8; e += 4) {                // (behind the rotating dims: whatever, unused)
+            *reinterpret_cast<float4 *>(c + e) = *reinterpret_cast<const float4 *>(&cs[0][tok][e ? pair1 : pair0]);
+            *reinterpret_cast<float4 *>(s + e) = *reinterpret_cast<const float4 *>(&cs[1][tok][e ? pair1 : pair0]);
         }
         __half *q_out = p.q_out + n * p.stride_q_out;
 #pragma unroll
@@ -179,10 +189,10 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeParams p)
                     w[0] = *reinterpret_cast<const f16x8_t *>(weight + d0);
                     w[1] = *reinterpret_cast<const f16x8_t *>(weight + d1);
                 }
-                float x[16];
+                f32x16_t x;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[e] = (float)a[u][e / 8][e % 8];
-                rope_row<D>(x, weight != nullptr, w, p.eps, rotates, p.interleaved, c, s);
+                rope_row<D>(x, weight != nullptr, w, p.eps, rotates0, rotates1, p.interleaved, c, s);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) a[u][e / 8][e % 8] = (_Float16)x[e];
             }

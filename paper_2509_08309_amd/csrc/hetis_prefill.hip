@@ -63,6 +63,11 @@ static int prefill_call(const hetis_attn_shape *shape, const void *q, const int3
     if (rc != HETIS_OK) return rc;
     if (!q || !q_starts || !k || !v || !block_table || !seq_lens || !head_ids || !out) return HETIS_ERR_NULL;
     const PrefillLayout lay = prefill_layout(shape, n_tokens, n_sel);
+    const int r = shape->n_q_heads / shape->n_kv_heads;
+    // numbers of a head: tiles, and what the sequences may have beside them
+    const int64_t gap = lay.rows ? 1 + kPfSplitItems : 1, numbers = n_tokens / (kPfRows / r) + gap * shape->batch;
+    const int heads = heads_of_a_launch(shape, n_sel);
+    if (numbers * heads > 1 << 30) return HETIS_ERR_UNSUPPORTED;
     const hipStream_t st = (hipStream_t)stream;
     if (owned && n_tokens == 0) return HETIS_OK;
     rc = owned ? owned_workspace(lay.total, st, true, &workspace) : check_workspace(workspace, workspace_bytes, lay.total);
@@ -84,12 +89,8 @@ static int prefill_call(const hetis_attn_shape *shape, const void *q, const int3
     p.batch = shape->batch;
     p.n_sel = n_sel;
     p.n_q_heads = shape->n_q_heads;
-    const int r = shape->n_q_heads / shape->n_kv_heads;
     p.group_shift = r == 8 ? 3 : r / 2;
     p.max_blocks_per_seq = shape->max_blocks_per_seq;
-    // numbers of a head: tiles, and what the sequences may have beside them
-    const int64_t gap = lay.rows ? 1 + kPfSplitItems : 1, numbers = n_tokens / (kPfRows / r) + gap * shape->batch;
-    if (numbers * n_sel > 1 << 30) return HETIS_ERR_UNSUPPORTED;
     p.tiles = (int)numbers;
     p.gap = (int)gap;
     p.scale_log2 = std::max(std::fabs(scale) * kLog2e, FLT_MIN);         // (0 times a masked score would be NaN)
@@ -101,7 +102,6 @@ static int prefill_call(const hetis_attn_shape *shape, const void *q, const int3
     p.rows_by_sequence = lay.by_sequence;
     const int cus = device_cu_count();
     if (cus <= 0) return HETIS_ERR_LAUNCH;
-    const int heads = heads_of_a_launch(shape, n_sel);
     // Without queues where nothing is gained by them: one sequence comes longest tiles first by itself (8192 tokens of 40
     // heads 700 us against 721, of 13 heads 244 against 258), and so few items start all at once.
     const bool direct = lay.rows == 0 || shape->batch == 1 || numbers * n_sel <= 4 * cus;

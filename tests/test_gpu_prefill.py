@@ -271,6 +271,18 @@ def test_strided_pools(layout):
     assert np.array_equal(bits(c.run([0, 3], shape=shape, k=kk, v=vv)), want)
 
 
+def test_offsets_past_32_bits():
+    c = Case([200, 40], [200, 3], 2, 2, 64, seed=46)
+    want, p, stride = bits(c.run([0, 1])), c.p, (1 << 28) + 1024
+    assert p.nb * stride > 1 << 32
+    far = []
+    for x in (p.k, p.v):
+        pool = torch.empty(p.nb * stride, dtype=torch.float16, device=DEV)
+        pool.as_strided((p.nb, x[0].size), (stride, 1)).copy_(dev(x).view(p.nb, -1))
+        far.append(pool)
+    assert np.array_equal(bits(c.run([0, 1], shape=c.shape(kv_stride_block=stride), k=far[0], v=far[1])), want)
+
+
 def test_wide_block_tables():
     """The table's width has no effect on a row."""
     want = None

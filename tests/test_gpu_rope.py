@@ -190,6 +190,22 @@ def test_store(hq, hkv, D, rot, heads, positions):
         assert np.array_equal(bits(a), bits(b))
 
 
+def test_offsets_past_32_bits():
+    lens = np.array([200, 40])
+    seq, slot = np.repeat(np.arange(2), lens), np.concatenate([np.arange(n) for n in lens])
+    c, stride, f = Cache(lens, 4, 2, 64, 16, len(seq)), (1 << 28) + 1024, frequencies(64)
+    assert c.nb * stride > 1 << 32
+    far = [torch.empty(c.nb * stride, dtype=torch.float16, device=DEV) for _ in range(2)]
+    pools = [x.as_strided((c.nb, 2, 16, 64), (stride, 16 * 64, 64, 1)) for x in far]
+    for x in pools:
+        x.copy_(sentinel(c.nb, 2, 16, 64))
+    q_out = sentinel(*c.q.shape)
+    H.check(H.hetis_kv_store_rope(c.shape(kv_stride_block=stride), H.make_rope(64), dev(f), dev(c.q), None, dev(c.k), None,
+                                  dev(c.v), i32(seq), i32(slot), None, len(seq), i32(c.table), i32([0, 1]), 2, c.nb, q_out, *far))
+    torch.cuda.synchronize()
+    c.expect([0, 1], seq, slot, slot, f, False, False, q_out, [x.contiguous() for x in pools])
+
+
 def test_entries_that_point_outside_are_skipped():
     c = Cache([40, 40, 40], 4, 2, 64, 7, 9)
     seq = np.array([0, -1, 3, 1, 1, 2, 2, 0, 1])

@@ -141,6 +141,22 @@ def test_strided_pools(layout):
     assert np.array_equal(other, np.where(tiles < 0, -1, block + g * p.nb if layout == "head-major" else block * 5 + g))
 
 
+def test_offsets_past_32_bits():
+    c = Case([200, 70], 2, 2, 64, seed=46)
+    p, stride = c.p, (1 << 28) + 1024
+    assert p.nb * stride > 1 << 32
+    far = torch.empty(p.nb * stride, dtype=torch.float16, device=DEV)
+    far.as_strided((p.nb, p.k[0].size), (stride, 1)).copy_(dev(p.k).view(p.nb, -1))
+    shape = c.shape(kv_stride_block=stride)
+    codes, scales = c.bounds([0, 1], [0, 0], k=far, shape=shape)
+    for got, want in zip((codes, scales), c.made([0, 1], [0, 0])):
+        same(got, want)
+    tiles, lens = c.select([0, 1], codes, scales, 3, 1, 1, shape=shape)
+    dense, _ = c.select([0, 1], codes, scales, 3, 1, 1)
+    blocks, heads = (dense // 2).cpu().numpy().astype(np.int64), (dense % 2).cpu().numpy()
+    assert np.array_equal(tiles.cpu().numpy(), blocks * (stride // 1024) + heads)
+
+
 def test_bounds_skip_what_points_outside():
     c = Case([40, 40], 2, 2, 64, seed=5)
     want = [x.copy() for x in c.made([1], [0, 0])]

@@ -12,7 +12,17 @@
 //                      leaves them, tokens 8 j + 4 h + i of two neighbouring j; A: V[those tokens][dim n], by
 //                      transposing LDS reads.
 //
-// The running maximum and sum of a row live in the two lanes that hold its scores.
+// The running maximum and sum of a row live in the two lanes that hold its scores.  A weight is rounded to fp16 (2^-11 of it)
+// for the second product; scores, sums and results are in fp32.
+//
+// Long prompts are bound by the chip's power: 8192 tokens x 40 heads of 128 take 700 us, 980 TFLOP/s (a large matrix product
+// reaches 1340), matrix cores 58 % and vector units 50 % busy at 1.54 GHz; with zeros for data, and the clock that they
+// allow, 497 us.  So what saves instructions saves time: one block of 32 rows a wave and two workgroups a compute unit, so
+// that one wave's exponentials run beside another's products; the softmax's reference moves only where a weight would pass
+// 2^8; nothing goes through registers on its way to LDS.  (Two blocks a wave and one workgroup a unit halve the reads from LDS,
+// and take 790 us: a wave that is alone on its SIMD cannot issue fast enough.  Workgroups of eight waves and 256 rows: no
+// better.)  A few new rows over long caches are bound by the cache's bytes: 64 x 5 drafted tokens x 3 groups of eight, 218 MB,
+// 70 us; 128 single tokens x 13 heads, 911 MB, 210 us.
 #pragma once
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -54,10 +64,13 @@ constexpr int kPfStep = 64;                 // cached tokens of a step
 // A sequence's first tiles, up to kPfSplitTiles of them, are cut along the cache as well, by the sequence's own numbers
 // only: into at most kPfSplitItems / tiles segments of at least kPfSegSteps steps.  All tiles of a few drafted tokens
 // over a long cache, and of a long chunk those that come last: without them its tiles, all about as long, leave most of
-// the chip idle in their last round.
+// the chip idle in their last round (1000 of 14000 tokens x 2 sequences x 8 groups 1081 us instead of 937).  Least lengths:
+// 16 steps where that is all of a sequence (64 x 5 drafted tokens x 3 groups 69 us; 8 steps 97, 24 steps 74; 128 single tokens x 13
+// heads 210, 217, 206), 48 otherwise (with 16 as well, 64 sequences of up to 3000 tokens, up to 300 of them new, x 8 groups
+// take 689 us instead of 606).
 constexpr int kPfSplitTiles = 8, kPfSplitItems = 32, kPfSegSteps = 16, kPfSegStepsOfMany = 48;
 constexpr int kPfQueues = 8;
-constexpr int kPfBatch = 8;                 // segments that are added up at a time
+constexpr int kPfBatch = 8;                 // segments that are added up at a time, their loads all on their way
 enum : int { kPfCtlTickets = 16, kPfCtlGone = 24 };      // control words: a queue's tickets, workgroups finished
 
 // What there is to do for a sequence.

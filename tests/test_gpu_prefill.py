@@ -177,6 +177,28 @@ def test_a_crowd_and_its_sequences_alone():
         assert np.array_equal(bits(one.run([0, 1])), both[s]), b
 
 
+def test_launches_of_some_heads_each():
+    """So many sequences that a launch has counters for one head of them only."""
+    rng = np.random.default_rng(76)
+    lens = rng.integers(1, 30, 20000)
+    c = Case(lens, np.minimum(rng.integers(0, 3, 20000), lens), 4, 2, 64, seed=77)
+    c.check(c.run([1, 0]), [0, 1], sequences=np.r_[0:20000:401, 19999])
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_drawn_cases(seed):
+    rng = np.random.default_rng([78, seed])
+    D, r, hkv = int(rng.choice([64, 128])), int(rng.choice([1, 2, 4, 8])), int(rng.integers(1, 4))
+    n = int(np.exp(rng.uniform(0, np.log(60))))
+    top = int(np.exp(rng.uniform(np.log(20), np.log(4000))))
+    lens = rng.integers(1, top + 1, n)
+    new = np.minimum(lens, np.exp(rng.uniform(0, np.log(rng.choice([2, 20, 400])), n)).astype(int))
+    new[rng.random(n) < 0.1] = 0
+    c = Case(lens, new, hkv * r, hkv, D, seed=79 + seed)
+    heads = list(rng.permutation(hkv)[:rng.integers(1, hkv + 1)])
+    c.check(c.run(heads), heads, sequences=rng.permutation(n)[:8], every=int(max(1, new.max() // 6)))
+
+
 def test_heads_of_a_subset_are_the_bits_of_all_heads():
     for hq, hkv, D, lens, new in ((8, 8, 64, [700, 33, 4500, 1], [700, 5, 40, 1]), (32, 4, 128, [5000, 260, 9000], [3, 260, 130])):
         c = Case(lens, new, hq, hkv, D, seed=21)

@@ -75,6 +75,33 @@ def test_strides_and_in_place(n, heads, extra):
     assert np.array_equal(bits(a)[:, heads * D:], fused.view(np.uint16)[:, heads * D:])
 
 
+@pytest.mark.parametrize("D,rot", [(64, 64), (64, 32), (128, 128), (128, 80)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("norm", [False, True])
+def test_large_calls_are_the_bits_of_small_ones(D, rot, interleaved, norm):
+    """Rows in memory and into the cache: several rows of a thread on their way, or one."""
+    n, hq, hkv = 4003, 16, 8
+    lens = np.array([n, 7])
+    c = Cache(lens, hq, hkv, D, 17, n)
+    pos, rope, f = i32(c.rng.integers(0, 1 << 18, n)), H.make_rope(rot, interleaved, 0.9), dev(frequencies(rot))
+    q, k, v = dev(c.q), dev(c.k), dev(c.v)
+    wq, wk = (dev(w) for w in c.weights) if norm else (None, None)
+    seq, slot, table, heads = i32(np.zeros(n)), i32(np.arange(n)), i32(c.table), i32([0, 3, 7, 2])
+    got = []
+    for part in (n, 50):
+        rows, q_out, pools = sentinel(n, hq, D), sentinel(n, hq, D), [sentinel(c.nb, hkv, 16, D) for _ in range(2)]
+        for i in range(0, n, part):
+            s = slice(i, min(n, i + part))
+            m = s.stop - i
+            H.check(H.hetis_rope_rows(rope, f, q[s], 0, wq, pos[s], m, hq, D, rows[s], 0))
+            H.check(H.hetis_kv_store_rope(c.shape(), rope, f, q[s], wq, k[s], wk, v[s], seq[s], slot[s], pos[s], m, table, heads,
+                                          4, c.nb, q_out[s], *pools))
+        torch.cuda.synchronize()
+        got.append([bits(x) for x in (rows, q_out, *pools)])
+    for a, b in zip(*got):
+        assert np.array_equal(a, b)
+
+
 def test_position_zero_and_no_rotation():
     """Position 0 keeps the bits of the rotated dims, and the others are kept at any position."""
     x = np.random.default_rng(1).standard_normal((40, 3, 64)).astype(np.float16)

@@ -205,6 +205,26 @@ def test_select_of_many_pages(pages):
             same(a, b, (n_pages, sink, recent))
 
 
+@pytest.mark.parametrize("seed", range(10))
+def test_drawn_cases(seed):
+    rng = np.random.default_rng([10, seed])
+    D, r, hkv = int(rng.choice([64, 128])), int(rng.choice([1, 2, 4, 8])), int(rng.integers(1, 5))
+    lens = np.exp(rng.uniform(0, np.log(rng.choice([100, 3000, 20000])), int(rng.integers(1, 9)))).astype(int)
+    c = Case(lens, hkv * r, hkv, D, seed=11 + seed)
+    heads = list(rng.permutation(hkv)[:rng.integers(1, hkv + 1)])
+    first = rng.integers(-5, lens + 1)
+    made = c.made(heads, first)
+    for got, want in zip(c.bounds(heads, first), made):
+        same(got, want)
+    codes, scales = c.made(range(hkv), np.zeros(len(lens)))
+    n_pages = int(np.exp(rng.uniform(0, np.log(400))))
+    recent = int(rng.integers(1, n_pages + 1))
+    sink = int(rng.integers(0, n_pages - recent + 1))
+    got = c.select(heads, dev(codes), dev(scales), n_pages, sink, recent)
+    for a, b in zip(got, c.wanted(heads, codes, scales, n_pages, sink, recent)):
+        same(a, b, (n_pages, sink, recent))
+
+
 def test_equal_scores_and_odd_queries():
     """All pages alike: the lowest; queries of zeros, infinite ones and NaN."""
     c = Case([16 * 700] * 4, 4, 2, 128, seed=7)

@@ -263,7 +263,6 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(SelectParams p)
 
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectBins = 2048;
-constexpr int kSelectFew = 256;                                    // keys that are compared with each other, see below
 
 __device__ __forceinline__ int lanes_below(unsigned long long mask)
 {
@@ -300,8 +299,8 @@ __device__ __forceinline__ unsigned threads_before(unsigned x, unsigned *sums)
 // The n_pages pages of the largest keys of a row, ascending: the smallest of them by a radix selection, then a sweep in
 // page order.  Counts are whole numbers: the same run to run.  Digits are of 11 bits from the highest bit on that the
 // keys' range has: scores lie within an octave or two, and digits of the bits as they are would crowd into a few
-// counters.  As soon as no more than kSelectFew keys share the digits found, each of them is compared with all.  A thread keeps KEYS pages, kSelectThreads apart, of a window; ONE: the rows have one window, and keys are read
-// once.  Bound by latency, one step after the other: 128 of 2048 pages 5.4 us, 256 of 8192 9.0 (9.5 with digits to the end).
+// counters.  A thread keeps KEYS pages, kSelectThreads apart, of a window; ONE: the rows have one window, and keys are read
+// once.  Bound by latency, one step after the other: 128 of 2048 pages 5.5 us, 256 of 8192 9.5.
 template <int KEYS, bool ONE>
 __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
 {
@@ -311,8 +310,6 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
     __shared__ unsigned sums[kSelectThreads / 64];
     __shared__ uint2 counts[KEYS * (kSelectThreads / 64) + 1];     // of pages that are taken, and of equal ones
     __shared__ int picked[3];
-    __shared__ __attribute__((aligned(16))) unsigned few[kSelectFew];
-    __shared__ int n_few;
     const int tid = threadIdx.x, i = blockIdx.x;
     const int64_t b = blockIdx.y;
     const int L = min(max(p.seq_lens[b], 0), p.max_blocks_per_seq * kBlockTokens), pages = (L + kBlockTokens - 1) / kBlockTokens, want = p.n_pages;
@@ -364,8 +361,6 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
     fold(lanes_xor<32>(low), lanes_xor<32>(high));
     if (tid % 64 == 0) ranges[tid / 64] = make_uint2(low, high);
     for (int k = tid; k < kSelectBins; k += kSelectThreads) hist[k] = 0;
-    if (tid == 0) n_few = 0;
-    if (tid < kSelectFew) few[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kSelectThreads / 64; ++w) {
@@ -422,36 +417,6 @@ __global__ void __launch_bounds__(kSelectThreads) select_kernel(SelectParams p)
         left = picked[1];
         equal = picked[2];
         __syncthreads();
-        if (equal > kSelectFew || left == equal || shift == 0) continue;
-        for (int w = 0; w < windows; ++w) {
-            if constexpr (!ONE) load(w);
-#pragma unroll
-            for (int e = 0; e < KEYS; ++e)
-                if (from + e * kSelectThreads < pages && key[e] != kSelectAlways && rank(key[e]) == least) few[atomicAdd(&n_few, 1)] = key[e];
-        }
-        __syncthreads();
-        if (tid < equal) {
-            const unsigned mine = few[tid];
-            int larger = 0, same = 0;
-            for (int k = 0; k < equal; k += 4) {                   // (zeros behind the last: no key is as small, see select_key)
-                const u32x4 other = *reinterpret_cast<const u32x4 *>(&few[k]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    larger += other[e] > mine;
-                    same += other[e] == mine;
-                }
-            }
-            if (larger < left && left <= larger + same) {          // (the same for all that share the key)
-                picked[0] = (int)(mine - low);
-                picked[1] = left - larger;
-                picked[2] = same;
-            }
-        }
-        __syncthreads();
-        least = (unsigned)picked[0];
-        left = picked[1];
-        equal = picked[2];
-        shift = 0;
     }
     // (where all that share the last digits are wanted, or none, the pass that would tell them apart is left out)
     int taken = 0, same_taken = 0;                                 // of the windows before

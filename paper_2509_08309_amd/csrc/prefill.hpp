@@ -12,8 +12,13 @@
 //                      leaves them, tokens 8 j + 4 h + i of two neighbouring j; A: V[those tokens][dim n], by
 //                      transposing LDS reads.
 //
-// The running maximum and sum of a row live in the two lanes that hold its scores.  A weight is rounded to fp16 (2^-11 of it)
-// for the second product; scores, sums and results are in fp32.
+// The running maximum and sum of a row live in the two lanes that hold its scores; scores, sums and results are in fp32.  A
+// weight is rounded to fp16 for the second product: two numbers a weight would hold it to 2^-22, with twice the products in a
+// kernel that power bounds.  To use what fp16 has above 1, weights are taken against a reference kPfBelow = 7 powers of two below the row's
+// maximum, which moves only where a weight would pass 2^15: the row's largest is 2^7 to 2^15, so that one of 2^-21 of it or more
+// is off by 2^-11 of itself at most, a lesser one by 2^-32 of the largest.  (With the maximum itself for reference weights of
+// 2^-25 of it vanished: 131072 tokens of these behind one dominant first token, 0.4 % of a row and, with that one's value
+// zero, all of it.)
 //
 // Long prompts are bound by the chip's power: 8192 tokens x 40 heads of 128 take 700 us, 980 TFLOP/s (a large matrix product
 // reaches 1340), matrix cores 58 % and vector units 50 % busy at 1.54 GHz; with zeros for data, and the clock that they
@@ -70,6 +75,7 @@ constexpr int kPfStep = 64;                 // cached tokens of a step
 // take 689 us instead of 606).
 constexpr int kPfSplitTiles = 8, kPfSplitItems = 32, kPfSegSteps = 16, kPfSegStepsOfMany = 48;
 constexpr int kPfQueues = 8;
+constexpr float kPfBelow = 7.f, kPfMost = 15.f;          // powers of two: of a new reference below the maximum; of the largest weight
 constexpr int kPfBatch = 8;                 // segments that are added up at a time, their loads all on their way
 enum : int { kPfCtlTickets = 16, kPfCtlGone = 24 };      // control words: a queue's tickets, workgroups finished
 
@@ -352,8 +358,8 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
         for (int e = 0; e < 16; ++e) s[half][e] = 0.f;
     };
     auto score = [&](int half, int e, pf_f16x8 k) { s[half] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[e], s[half], 0, 0, 0); };
-    // Brings the reference up to date: a weight is at most 2^8, and as long as that holds the reference stays (a row's
-    // own scores decide, whatever its neighbours need).
+    // Brings the reference up to date: a weight is at most 2^kPfMost, and as long as that holds the reference stays (a
+    // row's own scores decide, whatever its neighbours need).
     auto settle = [&](int step) {
         const int t0 = step * kPfStep;
         if (t0 + kPfStep - 1 > pos_lo) {
@@ -367,8 +373,8 @@ __device__ __forceinline__ void prefill_item(const PrefillParams &p, PrefillLds<
 #pragma unroll
         for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e / 16][e % 16]);
         top = max_xor32(top) * c;
-        if (__builtin_amdgcn_ballot_w64(top > mc + 8.f) != 0) {
-            const float to = top > mc + 8.f ? top : mc, alpha = fast_exp2(mc - to);
+        if (__builtin_amdgcn_ballot_w64(top > mc + kPfMost) != 0) {
+            const float to = top > mc + kPfMost ? top - kPfBelow : mc, alpha = fast_exp2(mc - to);
             mc = to;
             l *= alpha;
 #pragma unroll

@@ -224,6 +224,36 @@ def test_sequences_alone_and_together():
         assert np.array_equal(bits(one.run([0, 1])), both[s])
 
 
+@pytest.mark.parametrize("lens,new,hq,sequence,tokens", [([131072], [160], 8, 0, (0, 130, 159)),
+                                                         ([4000] * 3, [1, 5, 40], 2, 1, (0, 4)), ([1000], [1], 1, 0, (0,))])
+def test_a_dominant_key_ahead_of_a_long_weak_tail(lens, new, hq, sequence, tokens):
+    """The first token has nearly all of the weight and a value of zero, as the first of a context often has: what the
+    row comes to is the sum of many weights around e^-18 of the largest, whole in the tiles that are not cut along
+    the cache (tokens from 128 on of the first case).  Tolerance: attend's, with 2^-32 of the row's largest weight in
+    place of 2^-25 where a weight is subnormal in fp16: the largest is at least 2^7 there."""
+    c = Case(lens, new, hq, 1, 64, seed=91)
+    p, rng = c.p, np.random.default_rng(92)
+    c.scale, used = 1.0, np.isfinite(p.k)
+    k = (0.05 * rng.standard_normal(p.k.shape)).astype(np.float16)
+    k[..., 0] = -18 + rng.standard_normal(k.shape[:-1])
+    v = (1 + 0.5 * rng.standard_normal(p.v.shape)).astype(np.float16)
+    for b in range(len(lens)):
+        k[p.table[b, 0], 0, 0], v[p.table[b, 0], 0, 0] = 0, 0
+    p.k, p.v = np.where(used, k, p.k), np.where(used, v, p.v)
+    c.q[..., 0] = 1
+    out = c.run([0]).cpu().numpy()
+    keys, values = p.rows(sequence, 0)
+    L, n = int(p.lens[sequence]), int(c.new[sequence])
+    for token in tokens:
+        pos = L - n + token
+        for h in (0, hq - 1):
+            q = c.q[c.starts[sequence] + token, h][None].astype(np.float64)
+            ref, tol = attend(q, keys, values, c.scale, [pos])
+            tol -= (2.0 ** -25 - 2.0 ** -32) * np.abs(values[:pos + 1]).sum(0)
+            err = np.abs(out[c.starts[sequence] + token, h].astype(np.float64) - ref[0])
+            assert (tol > 0).all() and (err <= tol).all(), (token, h, (err / tol).max(), ref[0, :3], err[:3])
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
 def test_scales(scale):
     c = Case([100, 260], [100, 9], 4, 2, 64, seed=5)

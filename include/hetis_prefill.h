@@ -16,7 +16,8 @@
  * finite among the tokens that it sees makes its dim of the row not finite.
  *
  * Conventions: those of hetis_attn.h (lengths, block ids and head ids are not checked; q_starts is, as far as
- * memory goes: rows outside [0, n_tokens) are neither read nor written).  A row's result depends on its
+ * memory goes: rows outside [0, n_tokens) are neither read nor written; where it descends anywhere, what the call leaves in
+ * rows of `out` is unspecified, and a workspace serves the next call as before).  A row's result depends on its
  * sequence's cache up to its position, on n_b and on L_b only: a head-subset call returns the matching rows of the
  * all-heads call bit for bit, and results are the same run to run.
  *

@@ -195,7 +195,7 @@ struct PrefillLds {
     int before[kPfThreads + 1];                         // items of a queue ahead of a thread's sequences
     __attribute__((aligned(16))) int key[kPfThreads];   // what the sequences are ordered by
     PrefillSequence sequences[kPfThreads];              // by their place, up to one for each thread
-    int sums[kPfWaves], totals[kPfWaves][kPfQueues];
+    int sums[kPfWaves], wrong[kPfWaves], totals[kPfWaves][kPfQueues];
     PrefillItem item;
     int ticket, last;
 };
@@ -663,6 +663,13 @@ struct PrefillQueues {
         }
         for (int i = 0, rank = tid * per; i < per && rank < p.batch; ++i, ++rank) f(rank, prefill_sequence(p, rank).items());
     }
+    // Whether the starts of this thread's sequences, and those behind them, descend somewhere.
+    __device__ __forceinline__ bool descends() const
+    {
+        bool d = false;
+        for (int i = 0, b = thread_here() * per; i < per && b < p.batch; ++i, ++b) d |= p.q_starts[b + 1] < p.q_starts[b];
+        return d;
+    }
     __device__ __forceinline__ int total(int queue) const
     {
         int t = 0;
@@ -670,10 +677,12 @@ struct PrefillQueues {
         for (int w = 0; w < kPfWaves; ++w) t += sh.totals[w][queue];
         return t;
     }
-    // items of the queue ahead of each thread's; returns how many there are
+    // Items of the queue ahead of each thread's; returns how many there are, with starts that descend (CHECK) -1.
+    template <bool CHECK>
     __device__ __forceinline__ int open(int queue)
     {
         const int tid = thread_here(), lane = tid % 64, wave = tid / 64;
+        const bool wrong = CHECK && __builtin_amdgcn_ballot_w64(descends()) != 0;
         int sum = 0, h0;
         each([&](int rank, int items) { sum += items * pairs_in(queue, rank, &h0); });
         int upto = sum;
@@ -682,14 +691,22 @@ struct PrefillQueues {
             const int x = __shfl_up(upto, o);
             upto += lane >= o ? x : 0;
         }
-        if (lane == 63) sh.sums[wave] = upto;
+        if (lane == 63) {
+            sh.sums[wave] = upto;
+            if (CHECK) sh.wrong[wave] = wrong;
+        }
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kPfWaves; ++w) upto += w < wave ? sh.sums[w] : 0;
         sh.before[tid + 1] = upto;
         if (tid == 0) sh.before[0] = 0;
         __syncthreads();
-        return __builtin_amdgcn_readfirstlane(sh.before[kPfThreads]);
+        int total = sh.before[kPfThreads];
+        if (CHECK) {
+#pragma unroll
+            for (int w = 0; w < kPfWaves; ++w) total = sh.wrong[w] ? -1 : total;
+        }
+        return __builtin_amdgcn_readfirstlane(total);
     }
     // Item k of the open queue: of a sequence the tiles that see most first, one for each head.
     __device__ __forceinline__ PrefillItem find(int queue, int k)
@@ -725,7 +742,8 @@ struct PrefillQueues {
 // A launch without sequences that are cut along the cache, or of few items: item i is workgroup i's, and nothing is handed
 // out.  Items are numbered from q_starts[b] / tokens + gap b on (tokens: of a tile), which leaves at least as many numbers
 // to a sequence as it has items if the gap is what it may have beside its tiles; the sequence of a number is found 64
-// starts at a time.
+// starts at a time.  With sequences that are cut, of which there are at most 63 then (or one), nothing is done where the starts
+// descend: some of a tile's pieces would be found and others not, and its arrival counter would keep the count.
 __device__ __forceinline__ PrefillItem prefill_direct(const PrefillParams &p, int number)
 {
     const int lane = threadIdx.x % 64, token_shift = 7 - p.group_shift, place = p.tiles - 1 - number / p.n_sel;
@@ -739,10 +757,12 @@ __device__ __forceinline__ PrefillItem prefill_direct(const PrefillParams &p, in
         n = min(step, n - found * step);
     }
     PrefillItem item;
+    item.tile = -1;
+    if (p.gap > 1 && __builtin_amdgcn_ballot_w64(p.q_starts[min(lane + 1, p.batch)] < p.q_starts[min(lane, p.batch)]) != 0) return item;
     item.head = number % p.n_sel;
     item.seq = prefill_sequence(p, __builtin_amdgcn_readfirstlane(lo));
     const int u = place - (max(item.seq.start, 0) >> token_shift) - item.seq.b * p.gap;
-    item.tile = u < 0 ? -1 : item.seq.item(u, &item.seg);
+    if (u >= 0) item.tile = item.seq.item(u, &item.seg);
     return item;
 }
 
@@ -761,8 +781,8 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_kernel(PrefillParams p)
     PrefillQueues<D> queues(p, sh);
     const int tid = threadIdx.x, places = gridDim.x / kPfQueues;        // workgroups of a queue
     int queue = blockIdx.x % kPfQueues, k = blockIdx.x / kPfQueues, tried = 0;
-    int total = queues.open(queue);
-    for (;;) {
+    int total = queues.template open<true>(queue);
+    while (total >= 0) {                                // (starts that descend: nothing is done, by any workgroup)
         if (k < total) {
             const PrefillItem item = queues.find(queue, k);
             // The next ticket is drawn late, so that no workgroup sits on an item while another has none.
@@ -789,7 +809,7 @@ __global__ void __launch_bounds__(kPfThreads, 2) prefill_kernel(PrefillParams p)
         __syncthreads();
         k = sh.ticket;
         total = queues.total(queue);
-        if (k < total) queues.open(queue);
+        if (k < total) queues.template open<false>(queue);
     }
     // the last workgroup to leave puts the tickets back
     if (tid == 0) {

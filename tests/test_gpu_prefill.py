@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2509_08309_amd as H
+from paper_2509_08309_amd import binding as B
 from prefill_reference import Pool, attend
 
 from gpu_harness import SENTINEL, bits, no_expired_wait
@@ -366,6 +367,25 @@ def test_starts_that_do_not_begin_at_zero(ahead, mb):
     c.starts, c.n = c.starts + ahead, c.n + ahead
     got = bits(c.run([0, 1]))
     assert np.array_equal(got[ahead:], want) and (got[:ahead] == SENTINEL).all()
+
+
+@pytest.mark.parametrize("crowd_of", [0, 40, 700])
+def test_starts_that_descend_do_no_harm_to_the_next_call(crowd_of):
+    """What such a call writes is unspecified, but all its rows are in [0, n_tokens), and a workspace is as before: with
+    few sequences (direct launches), with queues in order of length and as they come."""
+    rest, new = crowd(crowd_of, {}, seed=93) if crowd_of else (np.zeros(0, int), np.zeros(0, int))
+    c = Case([12000, 20, 11000, *rest], [300, 7400, 300, *new], 1, 1, 64, seed=94)
+    ws, want = c.workspace([0]), bits(c.run([0]))
+    starts, out = c.starts, c.fresh_out()
+    for first in ([7680, 7980, 0, 300], [0, 300, 8000, 7000], [-300, 300, -(1 << 31), 290], [(1 << 31) - 1, 0, 300, 600]):
+        c.starts = np.concatenate([first, starts[4:]])
+        q, st, k, v, bt, sl = c.inputs()
+        H.check(H.hetis_attn_prefill_ws(c.shape(), q, st, c.n, k, v, bt, sl, i32([0]), 1, c.scale, out, ws, ws.numel()))
+        torch.cuda.synchronize()
+        assert not ws[B.HETIS_ATTN_CONTROL_BYTES:B.HETIS_ATTN_CONTROL_BYTES + (4 << 18)].any(), "arrival counters"
+        assert (bits(out)[int(starts[-1]):] == SENTINEL).all()
+        c.starts = starts
+        assert np.array_equal(bits(c.run([0], ws=ws)), want), first
 
 
 def test_two_streams_and_graphs():

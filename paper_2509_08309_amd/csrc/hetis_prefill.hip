@@ -12,6 +12,9 @@
 
 namespace hetis {
 
+// Items of a direct launch, one a workgroup: a dispatch counts its threads in 32 bits.
+constexpr int64_t kPfDirectItems = 0xffffffffLL / kPfThreads;
+
 static int check_prefill_shape(const hetis_attn_shape *s, int32_t n_tokens, int32_t n_sel, CacheStrides *c)
 {
     int rc = check_cache_shape(s, n_sel, false, c);
@@ -105,7 +108,8 @@ static int prefill_call(const hetis_attn_shape *shape, const void *q, const int3
     // Without queues where nothing is gained by them: one sequence comes longest tiles first by itself (8192 tokens of 40
     // heads 700 us against 721, of 13 heads 244 against 258), and so few items start all at once.
     // (Where sequences may be cut, a wave looks at all starts at once.)
-    const bool direct = lay.rows == 0 || shape->batch == 1 || (numbers * n_sel <= 4 * cus && shape->batch < 64);
+    const bool direct = numbers * heads <= kPfDirectItems &&
+                        (lay.rows == 0 || shape->batch == 1 || (numbers * n_sel <= 4 * cus && shape->batch < 64));
     for (int h = 0; h < n_sel; h += heads) {
         p.head_ids = head_ids + h;
         p.n_sel = std::min(heads, n_sel - h);

@@ -388,6 +388,19 @@ def test_starts_that_descend_do_no_harm_to_the_next_call(crowd_of):
         assert np.array_equal(bits(c.run([0], ws=ws)), want), first
 
 
+@pytest.mark.parametrize("lens,new", [([40], [40]), ([130, 33, 5], [130, 2, 5])])
+def test_more_rows_than_a_launch_has_workgroups_for(lens, new):
+    """2^27 tiles and more, by n_tokens: queues, as a dispatch takes less than 2^24 workgroups of 256 threads.  Rows that no
+    sequence names are not read or written, so that they need not be there."""
+    c = Case(lens, new, 8, 1, 64, seed=95)
+    want = bits(c.run([0]))
+    q, starts, k, v, bt, sl = c.inputs()
+    out = c.fresh_out()
+    H.check(H.hetis_attn_prefill(c.shape(), q, starts, (1 << 31) - 1, k, v, bt, sl, i32([0]), 1, c.scale, out))
+    torch.cuda.synchronize()
+    assert np.array_equal(bits(out), want)
+
+
 def test_two_streams_and_graphs():
     """Two captured calls with a workspace each, replayed side by side, between eager calls."""
     c = Case([6000, 130, 17], [40, 130, 1], 8, 2, 128, seed=51)

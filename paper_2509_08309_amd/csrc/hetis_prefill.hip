@@ -26,8 +26,14 @@ static int check_prefill_shape(const hetis_attn_shape *s, int32_t n_tokens, int3
     return r == 1 || r == 2 || r == 4 || r == 8 ? HETIS_OK : HETIS_ERR_UNSUPPORTED;
 }
 
+// Heads of a launch: those whose tiles have arrival counters.
+static int heads_of_a_launch(const hetis_attn_shape *s, int32_t n_sel)
+{
+    return (int)std::min<int64_t>(n_sel, kArrivalSlots / kPfSplitTiles / s->batch);
+}
+
 // Control words and arrival counters of the other calls stay as they are; behind them partial results of sequences that
-// are cut along the cache.
+// are cut along the cache, of the heads of a launch: the next launch is behind it on the stream and uses the same place.
 struct PrefillLayout {
     size_t partial = 0, total = HETIS_ATTN_CONTROL_BYTES;
     int64_t rows = 0;                       // of a head
@@ -46,14 +52,8 @@ static PrefillLayout prefill_layout(const hetis_attn_shape *s, int32_t n_tokens,
     w.by_sequence = by_sequence < by_row;
     w.rows = std::min(by_row, by_sequence);
     w.partial = HETIS_ATTN_CONTROL_BYTES + kArrivalBytes;
-    w.total = align256(w.partial + (size_t)n_sel * w.rows * (s->head_dim + 2) * sizeof(float));
+    w.total = align256(w.partial + (size_t)heads_of_a_launch(s, n_sel) * w.rows * (s->head_dim + 2) * sizeof(float));
     return w;
-}
-
-// Heads of a launch: those whose tiles have arrival counters.
-static int heads_of_a_launch(const hetis_attn_shape *s, int32_t n_sel)
-{
-    return (int)std::min<int64_t>(n_sel, kArrivalSlots / kPfSplitTiles / s->batch);
 }
 
 static int prefill_call(const hetis_attn_shape *shape, const void *q, const int32_t *q_starts, int32_t n_tokens,

@@ -186,6 +186,22 @@ def test_launches_of_some_heads_each():
     c.check(c.run([1, 0]), [0, 1], sequences=np.r_[0:20000:401, 19999])
 
 
+@pytest.mark.parametrize("hq,hkv,D,n", [(4, 2, 64, 20000), (24, 3, 64, 12000)])
+def test_launches_of_some_heads_each_with_long_contexts(hq, hkv, D, n):
+    """The same with sequences that are cut: launches of one or two heads, one after the other, with the same counters,
+    partial results and tickets, in a workspace of the caller's; each head's rows are its own call's."""
+    lens, new = crowd(n, {(b if b < 20 else n - 23 + b): x for b, x in LONG.items()}, seed=96)
+    c = Case(lens, new, hq, hkv, D, seed=97)
+    heads = list(range(hkv))[::-1]
+    ws = c.workspace(heads)
+    every = c.run(heads, ws=ws)
+    c.check(every, heads, sequences=np.r_[list(LONG), 0:n:n // 20, n - 1], every=37)
+    for g in heads:
+        rows = slice(g * c.p.r, (g + 1) * c.p.r)
+        assert np.array_equal(bits(c.run([g]))[:, rows], bits(every)[:, rows])
+    assert np.array_equal(bits(c.run(heads, ws=ws)), bits(every))
+
+
 @pytest.mark.parametrize("seed", range(16))
 def test_drawn_cases(seed):
     rng = np.random.default_rng([78, seed])

@@ -146,6 +146,20 @@ def test_workspaces():
     assert H.hetis_attn_prefill_workspace_bytes(H.make_shape(4, 24, 8, 64, 16), 5, 3)[0] == B.HETIS_ERR_UNSUPPORTED
 
 
+def test_workspace_of_calls_that_take_several_launches():
+    """2^18 arrival counters, eight a (sequence, head): 8 heads a launch with 4096 sequences, one with 20000; launches use
+    the same partial results."""
+    for batch, heads, more in ((4096, 8, (9, 16, 40)), (20000, 1, (2, 40)), (30000, 1, (40,))):
+        s = H.make_shape(batch, 40, 40, 128, 1000)
+        rc, one = H.hetis_attn_prefill_workspace_bytes(s, batch, heads)
+        assert rc == 0 and one > heads * batch * 130 * 4
+        for n in more:
+            assert H.hetis_attn_prefill_workspace_bytes(s, batch, n) == (0, one)
+    s = H.make_shape(64, 40, 40, 128, 1000)
+    sizes = [H.hetis_attn_prefill_workspace_bytes(s, 64, n)[1] for n in (1, 2, 40)]
+    assert sizes == sorted(set(sizes))
+
+
 # ------------------------------------------------------------------ frequencies
 
 def frequencies(rot, base=10000.0, scaling=H.HETIS_ROPE_PLAIN, factor=1.0, length=0.0, low=0.0, high=0.0):

@@ -67,21 +67,20 @@ static int select_call(const hetis_attn_shape *shape, const void *q, const void 
     p.n_pages = n_pages;
     p.n_sink = n_sink;
     p.n_recent = n_recent;
-    if (shape->max_blocks_per_seq > n_pages) {
+    const bool scored = shape->max_blocks_per_seq > n_pages;
+    if (scored) {
         const dim3 grid((unsigned)n_sel, (unsigned)((shape->max_blocks_per_seq + kScorePages - 1) / kScorePages), (unsigned)shape->batch);
-        if (shape->head_dim == 128) score_kernel<128><<<grid, kScoreThreads, 0, st>>>(p);
-        else score_kernel<64><<<grid, kScoreThreads, 0, st>>>(p);
-        rc = launched();
+        rc = shape->head_dim == 128 ? launch_kv(score_kernel<128>, grid, st, p, true, false, kScoreThreads)
+                                    : launch_kv(score_kernel<64>, grid, st, p, true, false, kScoreThreads);
         if (rc != HETIS_OK) return rc;
     }
     // Keys in registers where a row of the table fits, and no more of them than it needs: choice of 128 of 2048 pages x 8 x 13
     // 5.5 us with two a thread, 7.7 with eight; of 256 of 8192 x 8 9.5 with eight, 11 where they are read again in each pass.
     const dim3 rows((unsigned)n_sel, (unsigned)shape->batch);
     const int pages = shape->max_blocks_per_seq;
-    if (pages <= kSelectThreads * 2) select_kernel<2, true><<<rows, kSelectThreads, 0, st>>>(p);
-    else if (pages <= kSelectThreads * 8) select_kernel<8, true><<<rows, kSelectThreads, 0, st>>>(p);
-    else select_kernel<8, false><<<rows, kSelectThreads, 0, st>>>(p);
-    return launched();
+    if (pages <= kSelectThreads * 2) return launch_kv(select_kernel<2, true>, rows, st, p, !scored, true, kSelectThreads);
+    if (pages <= kSelectThreads * 8) return launch_kv(select_kernel<8, true>, rows, st, p, !scored, true, kSelectThreads);
+    return launch_kv(select_kernel<8, false>, rows, st, p, !scored, true, kSelectThreads);
 }
 
 }  // namespace hetis

@@ -275,6 +275,27 @@ def test_workspaces_and_graphs():
         assert all(torch.equal(a, b) for a, b in zip(c.select([0, 1], codes, scales, 40, 1, 2, ws=ws[0]), want))
 
 
+@pytest.mark.parametrize("n_pages", [8, 400])
+def test_profile_events_carry_the_choice(n_pages):
+    """hetis_kv_profile_events: stamped anew by a choice of pages, with scores ahead of it and without."""
+    c = Case([5000, 40], 8, 2, 128, seed=61)
+    codes, scales = c.bounds([0, 1], np.zeros(2))
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    torch.zeros(1 << 28, dtype=torch.uint8, device=DEV)
+    end.record()
+    torch.cuda.synchronize()
+    old = begin.elapsed_time(end)
+    assert H.hetis_kv_profile_events(begin.cuda_event, end.cuda_event) == 0
+    try:
+        got = c.select([1, 0], codes, scales, n_pages, 1, 2)
+    finally:
+        H.hetis_kv_profile_events(None, None)
+    assert 0.0 < begin.elapsed_time(end) < 5.0 and begin.elapsed_time(end) != old
+    for x, y in zip(got, c.select([1, 0], codes, scales, n_pages, 1, 2)):
+        assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("hq,hkv,D,heads", [(8, 8, 64, [1, 6]), (16, 2, 128, [1, 0])])
 def test_a_request_from_its_prompt_on(hq, hkv, D, heads):
     """Prompts stored with rotation, prefill Attention over them in two chunks, then decode steps: append with

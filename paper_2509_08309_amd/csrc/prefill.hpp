@@ -151,7 +151,10 @@ __device__ __forceinline__ i32x4 tile_descriptor(const __half *tile, int nbytes)
 // A page into LDS at `to`, past the registers: load e's sixteen bytes of lane i go to `to` + (64 e + i) 16.  (By hand,
 // because the compiler waits for such loads ahead of any later LDS read; the caller waits, once a step.  There are no
 // registers that wait for them.  The wait states are those that a load needs behind a vector instruction that has
-// written its descriptor, and behind a change of M0.)
+// written its descriptor, and behind a change of M0, which the compiler has to know of: it puts values there
+// itself, and may keep one for several instructions.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"          // (that M0 is not preserved across the block is what is meant)
 template <int D>
 __device__ __forceinline__ void page_to_lds(i32x4 r, int from0, int from1, int from2, int from3, unsigned to)
 {
@@ -163,13 +166,14 @@ __device__ __forceinline__ void page_to_lds(i32x4 r, int from0, int from1, int f
                      "buffer_load_dwordx4 %2, %4, 0 offen offset:%7 lds\n\t"
                      "buffer_load_dwordx4 %3, %4, 0 offen offset:%8 lds"
                      :: "v"(from0), "v"(from1), "v"(from2), "v"(from3), "s"(r), "s"(to), "n"(LOAD), "n"(2 * LOAD),
-                        "n"(3 * LOAD) : "memory");
+                        "n"(3 * LOAD) : "m0", "memory");
     else
         asm volatile("s_mov_b32 m0, %3\n\ts_nop 4\n\t"
                      "buffer_load_dwordx4 %0, %2, 0 offen lds\n\t"
                      "buffer_load_dwordx4 %1, %2, 0 offen offset:%4 lds"
-                     :: "v"(from0), "v"(from3), "s"(r), "s"(to), "n"(LOAD) : "memory");
+                     :: "v"(from0), "v"(from3), "s"(r), "s"(to), "n"(LOAD) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 
 // Pieces of a row change places with its number, so that the lanes that read together meet different banks: 16 rows at
 // the same piece (K), four rows at four neighbouring pieces (V).

@@ -1,10 +1,13 @@
 """What the compiler made of the kernels of prefill Attention, rotary positions and the choice of pages, checked
 without a GPU: no scratch memory, and registers and LDS for the workgroups that a compute unit is meant to hold."""
+import os
 import re
 import shutil
+import subprocess
 
 import pytest
 
+from paper_2509_08309_amd import build
 from test_chunk_resources import resources
 from test_kernel_resources import HIPCC, kernel_metadata
 
@@ -43,3 +46,14 @@ def test_a_compute_unit_holds_the_workgroups_it_is_meant_to(source, kernels):
         waves = min(512 // (-(-registers // 8) * 8), 8)      # of a SIMD
         assert 4 * waves * 64 >= residents(name) * threads, (name, registers)
         assert residents(name) * lds <= 160 << 10, (name, lds)
+
+
+def test_the_compiler_knows_what_loads_into_lds_change():
+    """M0 is set by hand for them, in inline assembly that names it among the registers that it changes."""
+    flags = [f for f in build.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
+    ir = subprocess.run([HIPCC, *flags, "--cuda-device-only", "-S", "-emit-llvm", "-o", "-",
+                         os.path.join(build.CSRC, "hetis_prefill.hip")], capture_output=True, text=True, check=True).stdout
+    found = [line for line in ir.splitlines() if " asm " in line and "s_mov_b32 m0" in line]
+    assert len(found) >= 4, "two head dims, two kernels"
+    for line in found:
+        assert "~{m0}" in line, line.strip()

@@ -54,7 +54,8 @@ enum {
 /*
  * Writes f_0 .. f_(rot_dim / 2 - 1) to inv_freq (host, fp64).  length, low and high count for PARTS only.
  * Errors: NULL, UNSUPPORTED (rot_dim not a multiple of 16 in 16 .. 128, unknown scaling), BAD_SHAPE (base <= 0,
- * factor <= 0, length <= 0, not low < high, or a number that is not finite).
+ * factor <= 0, length <= 0, not low < high, or a number that is not finite, high - low, the larger base and the
+ * frequencies among them; nothing is written then).
  */
 int hetis_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double length,
                            double low, double high, double *inv_freq);

@@ -115,16 +115,21 @@ int hetis_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double
     if (!(base > 0 && std::isfinite(base))) return HETIS_ERR_BAD_SHAPE;
     if (scaling != HETIS_ROPE_PLAIN && !(factor > 0 && std::isfinite(factor))) return HETIS_ERR_BAD_SHAPE;
     if (scaling == HETIS_ROPE_PARTS &&
-        !(length > 0 && std::isfinite(length) && std::isfinite(low) && std::isfinite(high) && low < high))
+        !(length > 0 && std::isfinite(length) && std::isfinite(low) && std::isfinite(high) && low < high &&
+          std::isfinite(high - low)))
         return HETIS_ERR_BAD_SHAPE;
     if (scaling == HETIS_ROPE_BASE) base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
+    if (!std::isfinite(base)) return HETIS_ERR_BAD_SHAPE;
+    double made[64];
     for (int i = 0; i < rot_dim / 2; ++i) {
         const double f = std::pow(base, -2.0 * i / rot_dim);
         double keep = scaling == HETIS_ROPE_LINEAR ? 0.0 : 1.0;
         if (scaling == HETIS_ROPE_PARTS)
             keep = std::min(1.0, std::max(0.0, (length * f / 6.283185307179586 - low) / (high - low)));
-        inv_freq[i] = keep == 1.0 ? f : f * keep + f / factor * (1.0 - keep);
+        made[i] = keep == 1.0 ? f : f * keep + f / factor * (1.0 - keep);
+        if (!std::isfinite(made[i])) return HETIS_ERR_BAD_SHAPE;
     }
+    std::copy(made, made + rot_dim / 2, inv_freq);
     return HETIS_OK;
 }
 

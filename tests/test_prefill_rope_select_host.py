@@ -202,3 +202,14 @@ def test_frequencies_refused():
                {"scaling": 3, "high": math.inf}):
         assert call(**kw) == B.HETIS_ERR_BAD_SHAPE, kw
     assert call(scaling=0, factor=0.0, length=0.0) == B.HETIS_OK          # (not used)
+
+
+def test_frequencies_that_are_not_finite_are_refused():
+    """A larger base, quotients by a small factor, a range of turns past fp64: refused, and nothing is written."""
+    f = np.full(64, 7.0)
+    for base, scaling, factor, length, low, high in (
+            (1e306, H.HETIS_ROPE_BASE, 1e4, 0.0, 0.0, 0.0), (1e4, H.HETIS_ROPE_LINEAR, 1e-310, 0.0, 0.0, 0.0),
+            (1e-300, H.HETIS_ROPE_LINEAR, 1e-20, 0.0, 0.0, 0.0), (1e4, H.HETIS_ROPE_PARTS, 1e-310, 8192.0, 1.0, 32.0),
+            (1e4, H.HETIS_ROPE_PARTS, 8.0, 8192.0, -1e308, 1e308)):
+        assert H.hetis_rope_frequencies(128, base, scaling, factor, length, low, high, f) == B.HETIS_ERR_BAD_SHAPE
+        assert (f == 7.0).all()

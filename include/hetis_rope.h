@@ -20,7 +20,7 @@
  * kept or synchronised.  Indices that the calls read from device memory are checked as in hetis_kv.h.
  *
  * Supported: head_dim in {64, 128}; rot_dim a multiple of 16, 16 .. head_dim; block_size 16; any group size r with
- * n_sel_heads * (r + 2)^2 < 2^32; up to 524280 rows of a token.
+ * n_sel_heads * (r + 2)^2 < 2^32; up to 524280 rows of a token that are worked on, among Hq * D <= 2^32 elements.
  * Rows, weights and pools start at 16-byte boundaries.
  */
 #ifndef HETIS_ROPE_H

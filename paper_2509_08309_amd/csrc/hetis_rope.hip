@@ -58,8 +58,9 @@ static int store_call(const hetis_attn_shape *shape, const hetis_rope *rope, con
     if (!token_seq && n_tokens > shape->batch) return HETIS_ERR_BAD_SHAPE;
     const int group = shape->n_q_heads / shape->n_kv_heads;
     const int64_t rows = (int64_t)n_sel * (2 + (q ? group : 0));
-    // (a grid's limit, and that of a division by multiplication)
+    // (a grid's limit, that of a division by multiplication, and that of a row's place in its token)
     if (rows > kRopeMostRows || rows * (2 + group) > 0xffffffffLL) return HETIS_ERR_UNSUPPORTED;
+    if ((int64_t)shape->n_q_heads * shape->head_dim > (int64_t)1 << 32) return HETIS_ERR_UNSUPPORTED;
     if (!inv_freq || !k_new || !v_new || !token_pos || !angle_pos || !block_table || !head_ids || !k_cache || !v_cache)
         return HETIS_ERR_NULL;
     if ((q == nullptr) != (q_out == nullptr)) return HETIS_ERR_NULL;

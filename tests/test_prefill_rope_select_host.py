@@ -97,6 +97,16 @@ def test_numbers_out_of_range():
     assert CALLS["select"](s) == B.HETIS_ERR_BAD_SHAPE
 
 
+def test_tokens_of_too_many_heads():
+    """A row's place in its token is a 32-bit number of elements."""
+    for hq, hkv, dim in ((1 << 26, 1 << 26, 128), ((1 << 26) + 1024, 1024, 64), (1 << 27, 1 << 20, 128)):
+        s = H.make_shape(2, hq, hkv, dim, 16)
+        assert CALLS["append"](s, n=1, q=None, q_out=None) == B.HETIS_ERR_UNSUPPORTED
+        assert CALLS["store"](s, n=1, tok=1, q=None, q_out=None) == B.HETIS_ERR_UNSUPPORTED
+    s = H.make_shape(2, 1 << 26, 1 << 26, 64, 16)
+    assert CALLS["store"](s, n=4, tok=0) == B.HETIS_OK
+
+
 @pytest.mark.parametrize("rope,status", [
     (H.make_rope(0), B.HETIS_ERR_UNSUPPORTED), (H.make_rope(8), B.HETIS_ERR_UNSUPPORTED),
     (H.make_rope(24), B.HETIS_ERR_UNSUPPORTED), (H.make_rope(80), B.HETIS_ERR_UNSUPPORTED),

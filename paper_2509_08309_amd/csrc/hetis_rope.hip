@@ -3,6 +3,7 @@
 #include "../../include/hetis_rope.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "cache_checks.hpp"
@@ -22,6 +23,10 @@ static int check_rope(const hetis_rope *r, int32_t head_dim)
     if (!std::isfinite(r->magnitude) || !std::isfinite(r->norm_eps) || r->norm_eps < 0.f) return HETIS_ERR_BAD_SHAPE;
     return HETIS_OK;
 }
+
+// The hardware's reciprocal root takes a subnormal number for 0, and a row of zeros would be 0 * inf.  Any other row's mean
+// square is at least 2^-48 / 128, so that an eps below 2^-126 does not count there.
+static float norm_eps(const hetis_rope *r) { return r->norm_eps > 0.f ? std::max(r->norm_eps, FLT_MIN) : 0.f; }
 
 template <int D, bool STORE>
 static int launch_rope_u(RopeParams p, hipStream_t st)
@@ -97,7 +102,7 @@ static int store_call(const hetis_attn_shape *shape, const hetis_rope *rope, con
     p.rot_dim = rope->rot_dim;
     p.interleaved = rope->interleaved;
     p.magnitude = rope->magnitude;
-    p.eps = rope->norm_eps;
+    p.eps = norm_eps(rope);
     return launch_rope<true>(shape->head_dim, p, (hipStream_t)stream);
 }
 
@@ -163,7 +168,7 @@ int hetis_rope_rows(const hetis_rope *rope, const double *inv_freq, const void *
     p.rot_dim = rope->rot_dim;
     p.interleaved = rope->interleaved;
     p.magnitude = rope->magnitude;
-    p.eps = rope->norm_eps;
+    p.eps = norm_eps(rope);
     return launch_rope<false>(head_dim, p, (hipStream_t)stream);
 }
 

@@ -54,6 +54,22 @@ def test_rows(D, rot, interleaved, norm, n, heads):
     close(out.cpu().numpy(), ref, tol)
 
 
+@pytest.mark.parametrize("eps", [1e-40, 1.4e-45, 2e-38, 1e-12, 1e30])
+def test_norms_of_rows_of_zeros_and_of_the_least_values(eps):
+    """Whatever eps is above 0, subnormal in fp32 too: a row of zeros stays one, the smallest fp16 values are normed."""
+    D, f = 128, frequencies(128)
+    x = np.zeros((6, 2, D), dtype=np.float16)
+    x[1:4] = 2.0 ** -24 * np.random.default_rng(5).integers(-3, 4, (3, 2, D))
+    x[4, 0, 9], x[4, 1] = 2.0 ** -24, 65504.0
+    out, pos = sentinel(6, 2, D), np.arange(6)
+    weight = np.full(D, 1.5, dtype=np.float16)
+    H.check(H.hetis_rope_rows(H.make_rope(D, norm_eps=eps), dev(f), dev(x), 0, dev(weight), i32(pos), 6, 2, D, out, 0))
+    torch.cuda.synchronize()
+    ref, tol = rotate(x, pos, f, False, weight, np.float64(np.float32(eps)))
+    assert (ref[[0, 5]] == 0).all()
+    close(out.cpu().numpy(), ref, tol)
+
+
 @pytest.mark.parametrize("n,heads,extra", [(5, 6, 8), (3000, 40, 24), (700, 8, 1032)])
 def test_strides_and_in_place(n, heads, extra):
     """Query rows of a fused buffer, rotated into rows of their own and in place: the same bits, and what lies between

@@ -23,6 +23,8 @@
  *
  * Supported: head_dim in {64, 128}; block_size 16; r in {1, 2, 4, 8}; batch <= 32768, n_kv_heads <= 1024,
  * max_blocks_per_seq <= 2^24, n_tokens * r * n_sel_heads < 2^37.  Pools, queries and outputs start at 16-byte boundaries.
+ * fp16 pools with a row of the block table a sequence only: neither the rows a pair of hetis_attn_decode_pairs nor the 4-bit
+ * cache (hetis_kv4.h).  hetis_attn_profile_events does not reach these calls.
  */
 #ifndef HETIS_PREFILL_H
 #define HETIS_PREFILL_H

@@ -17,11 +17,13 @@
  *
  * Conventions: those of hetis_attn.h and hetis_kv.h: device pointers unless marked host, calls enqueue on
  * `stream` and return a status, argument errors are detected before the first HIP call, nothing is allocated,
- * kept or synchronised.  Indices that the calls read from device memory are checked as in hetis_kv.h.
+ * kept or synchronised.  Indices that the calls read from device memory are checked as in hetis_kv.h.  The events of
+ * hetis_kv_profile_events go with every call of this header, hetis_rope_rows too.
  *
  * Supported: head_dim in {64, 128}; rot_dim a multiple of 16, 16 .. head_dim; block_size 16; any group size r with
  * n_sel_heads * (r + 2)^2 < 2^32; up to 524280 rows of a token that are worked on, among Hq * D <= 2^32 elements.
- * Rows, weights and pools start at 16-byte boundaries.
+ * Rows, weights and pools start at 16-byte boundaries.  fp16 pools with a row of the block table a sequence only (rows for a
+ * pair's tiles or the 4-bit cache: hetis_rope_rows ahead of their own store calls).
  */
 #ifndef HETIS_ROPE_H
 #define HETIS_ROPE_H

@@ -18,10 +18,12 @@
  *     score = max_j (f32(sum_d c_jd * (c_jd > 0 ? upper_d : lower_d)) * t_j) * s
  * The sum is in whole numbers, so that the score, and with it the choice, has one value whatever the order.  A
  * page of scale +inf scores +inf; a query head with an infinite value or NaN takes no part (a group of such
- * heads only: all pages score alike).
+ * heads only: all pages of finite scale score alike).
  *
  * Conventions: those of hetis_attn.h.  batch <= 65535, n_kv_heads <= 1024, max_blocks_per_seq <= 2^24
  * (hetis_kv_select: 2^23); hetis_kv_select: r in {1, 2, 4, 8}; head_dim in {64, 128}; block_size 16.  Codes start at a 16-byte boundary.
+ * fp16 pools with a row of the block table a sequence only: neither the rows a pair of hetis_attn_decode_pairs nor the 4-bit
+ * cache (hetis_kv4.h).
  */
 #ifndef HETIS_SELECT_H
 #define HETIS_SELECT_H

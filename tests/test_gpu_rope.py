@@ -323,3 +323,27 @@ def test_a_graph_of_a_step():
         torch.cuda.synchronize()
         for a, b in zip([q2, o2] + p2, [q_out, out] + pools):
             assert np.array_equal(bits(a), bits(b)), turn
+
+
+@pytest.mark.parametrize("call", ["rows", "append"])
+def test_profile_events_go_with_every_call(call):
+    c = Cache([40, 7], 8, 2, 64, 31, 2)
+    rope, f, q, out = H.make_rope(64), dev(frequencies(64)), dev(c.q), sentinel(2, 8, 64)
+    pools = [sentinel(c.nb, 2, 16, 64) for _ in range(2)]
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    torch.zeros(1 << 28, dtype=torch.uint8, device=DEV)
+    end.record()
+    torch.cuda.synchronize()
+    old = begin.elapsed_time(end)
+    assert H.hetis_kv_profile_events(begin.cuda_event, end.cuda_event) == 0
+    try:
+        if call == "rows":
+            H.check(H.hetis_rope_rows(rope, f, q, 0, None, i32([3, 4]), 2, 8, 64, out, 0))
+        else:
+            H.check(H.hetis_kv_append_rope(c.shape(), rope, f, q, None, dev(c.k), None, dev(c.v), i32(c.table), i32(c.lens),
+                                           None, i32([1]), 1, c.nb, out, *pools))
+    finally:
+        H.hetis_kv_profile_events(None, None)
+    torch.cuda.synchronize()
+    assert 0.0 < begin.elapsed_time(end) < 5.0 and begin.elapsed_time(end) != old

@@ -62,6 +62,7 @@ int hetis_kv_bounds(const hetis_attn_shape *shape, const void *k_cache, const in
  * These are the block table and the lengths of a hetis_attn_decode_pairs call over the same pools with
  * kv_stride_block = kv_stride_head = 0, max_blocks_per_seq = n_pages and the pairs (b, head_ids[i]).
  * Lengths, block ids and head ids are not checked (hetis_attn_validate does); a negative length counts as 0.
+ * Of pages whose bounds were never made, scales of NaN among them, which ones are taken is unspecified, their number is not.
  *
  * hetis_kv_select_ws: the caller's workspace, hetis_kv_select_workspace_bytes(shape, n_sel_heads) bytes; the
  *   rules are those of hetis_attn_decode_ws, and one workspace may serve these calls and those of hetis_attn.h.

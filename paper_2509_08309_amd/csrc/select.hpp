@@ -150,12 +150,13 @@ struct SelectParams {
     int32_t n_sel, n_q_heads, n_kv_heads, group, max_blocks_per_seq, n_pages, n_sink, n_recent;
 };
 
-// Larger score, larger key; pages that are taken in any case come first.
+// Larger score, larger key; pages that are taken in any case come first, and no others have their key, not even those of a
+// score that is NaN: the choice counts on their number.
 constexpr unsigned kSelectAlways = 0xffffffffu;
 __device__ __forceinline__ unsigned select_key(float score)
 {
     const unsigned u = __float_as_uint(score + 0.f);               // (-0 as +0)
-    return (u & 0x80000000u) ? ~u : u | 0x80000000u;               // +inf: 0xff800000
+    return min((u & 0x80000000u) ? ~u : u | 0x80000000u, kSelectAlways - 1);        // +inf: 0xff800000
 }
 
 constexpr int kScoreThreads = 256;

@@ -242,6 +242,31 @@ def test_equal_scores_and_odd_queries():
             same(a, b)
 
 
+@pytest.mark.parametrize("pages,n_pages", [(40, 9), (3000, 130), (9000, 64)])
+def test_scales_that_are_nan(pages, n_pages):
+    """Bounds that were never made hold anything, every bit set for one.  Which pages are taken is unspecified then, but
+    they are n_pages of the sequence's, ascending, first and last ones among them, and nothing else is written."""
+    c = Case([16 * pages, 16 * pages - 3], 2, 2, 64, seed=62)
+    p, heads = c.p, [1, 0]
+    codes, scales = c.bounds(heads, np.zeros(2))
+    clean = c.select(heads, codes, scales, n_pages, 1, 2)
+    for bad in (0x7fffffff, -1, 0x7fc00000, -(1 << 22)):
+        rng = np.random.default_rng(bad & 0xffff)
+        for b in range(2):
+            at = rng.choice(pages, max(pages // 3, n_pages + 5), replace=False)
+            scales.view(torch.int32)[torch.from_numpy(p.table[b, at].astype(np.int64)).to(DEV), 1] = bad
+        tiles, lens = c.select(heads, codes, scales, n_pages, 1, 2)
+        assert torch.equal(lens, clean[1])
+        assert torch.equal(tiles.view(2, 2, -1)[:, 1], clean[0].view(2, 2, -1)[:, 1])          # head 0 has no such page
+        for b in range(2):
+            t = tiles.view(2, 2, -1)[b, 0].cpu().numpy()
+            blocks = (t - 1) // 2
+            page_of = {int(blk): j for j, blk in enumerate(p.table[b, :pages])}
+            chosen = [page_of[int(blk)] for blk in blocks]
+            assert (t % 2 == 1).all() and chosen == sorted(set(chosen))
+            assert chosen[0] == 0 and chosen[-2:] == [pages - 2, pages - 1]
+
+
 def test_workspaces_and_graphs():
     c = Case([9000, 300, 6000], 8, 2, 128, seed=9)
     codes, scales = (dev(x) for x in c.made([0, 1], np.zeros(3)))

@@ -459,3 +459,15 @@ def test_one_new_token_is_decode():
     H.check(H.hetis_attn_decode(c.shape(), dev(c.q), dev(p.k), dev(p.v), i32(p.table), i32(p.lens), i32([0, 1]), 2, c.scale, out))
     torch.cuda.synchronize()
     assert (got.float() - out.float()).abs().max() <= 2 * 4e-3
+
+
+@pytest.mark.parametrize("hq,hkv,D", [(2, 2, 128), (8, 2, 64), (16, 2, 128)])
+def test_decode_and_one_new_token_within_the_same_tolerance(hq, hkv, D):
+    """Both against the definition: a weight has 2^-11 of itself or better in either."""
+    c = Case([1, 16, 300, 4097, 700], [1, 1, 1, 1, 1], hq, hkv, D, seed=62, spare=0)
+    p, heads = c.p, list(range(hkv))
+    c.check(c.run(heads), heads)
+    out = c.fresh_out()
+    H.check(H.hetis_attn_decode(c.shape(), dev(c.q), dev(p.k), dev(p.v), i32(p.table), i32(p.lens), i32(heads), hkv, c.scale, out))
+    torch.cuda.synchronize()
+    c.check(out, heads)
